@@ -22,6 +22,12 @@
  * and zscore for the online regime of scoring each token as it is generated
  * (Sec. 3.3), after which the step only selects and compacts.
  *
+ * Around the step stand the calls that fill and read the same cache:
+ * epikv_rope_table and epikv_rope (rotary positions), epikv_append (new keys
+ * and values into the pages, rotated on the way), epikv_attend (attention
+ * over the pages) and epikv_read (rows back as bf16).  The pages hold bf16
+ * rows or rows of 4 bits (epikv_kv_format); the step moves either.
+ *
  * Conventions shared by every entry point
  * ---------------------------------------
  * - Pointers are device pointers unless marked "host".  The caller owns
@@ -101,6 +107,23 @@ typedef enum epikv_compact_mode {
   EPIKV_COMPACT_REMAP = 2          /* epikv_compact_remap (table rewritten) */
 } epikv_compact_mode;
 
+/*
+ * How the pages hold a token's K or V row (epikv_cfg.kv_format).
+ *
+ * MXFP4: per KV head, blocks of 32 channels.  A block holds 32 e2m1 codes
+ * (sign, two exponent bits, one mantissa bit: 0, .5, 1, 1.5, 2, 3, 4, 6) and
+ * a scale byte s; a channel's value is its code's times 2^(s - 127), and NaN
+ * throughout a block with s = 255.  A row is n_kv_heads*head_dim/2 bytes of
+ * codes (two to a byte, the lower channel in the low half), then
+ * n_kv_heads*head_dim/32 scale bytes, heads outermost in both, padded to a
+ * multiple of 16 bytes and to 128 at least (the padding is never written):
+ * 4.25 bits a value.
+ */
+typedef enum epikv_kv_format {
+  EPIKV_KV_BF16 = 0,
+  EPIKV_KV_MXFP4 = 1
+} epikv_kv_format;
+
 #define EPIKV_MAX_BAND 32   /* band layers per call */
 #define EPIKV_MAX_WINDOW 256
 
@@ -130,13 +153,16 @@ typedef struct epikv_cfg {
   int32_t budget;       /* K >= 1: positions kept per sequence */
   int32_t recent;       /* R >= 0, or -1 for min(128, K/4) (App. D) */
   float ema_alpha;      /* EMA weight of the previous average, [0, 1] (paper: 0.9) */
+  int32_t kv_format;    /* epikv_kv_format of the pool's rows; the KV-vector
+                           signals read bf16 rows only (EPIKV_EINVAL_PARAM) */
 } epikv_cfg;
 
 /*
- * A paged bf16 KV pool.  The K (kv = 0) or V (kv = 1) row of the token in
+ * A paged KV pool.  The K (kv = 0) or V (kv = 1) row of the token in
  * slot s of page p at layer l starts at
  *     base + l*stride_layer + kv*stride_kv + p*stride_page + s*row_bytes
- * with row_bytes = n_kv_heads*head_dim*2: all KV heads of one token are one
+ * with row_bytes = n_kv_heads*head_dim*2 for bf16 rows (see epikv_kv_format
+ * for 4-bit ones): all KV heads of one token are one
  * contiguous row, heads outermost.  Strides are in bytes, multiples of 16,
  * and base is 16-byte aligned.  Valid page ids are [0, n_pages).
  */
@@ -150,7 +176,8 @@ typedef struct epikv_pool {
 
 /* Fill *cfg with the paper's setting: 32 layers, D = 4096, 8 KV heads x 128,
  * 16-token pages, Band A = 7 layers, Band B = 8 layers, w = 64, eps = 1e-6,
- * HS signal, z-score smoothing, R = min(128, K/4), EMA alpha = 0.9.  batch and budget are set
+ * HS signal, z-score smoothing, R = min(128, K/4), EMA alpha = 0.9, bf16
+ * rows.  batch and budget are set
  * to 1 and 4096.  Returns EPIKV_EINVAL_NULL if cfg is NULL. */
 int epikv_default_cfg(epikv_cfg* cfg);
 
@@ -159,6 +186,10 @@ const char* epikv_strerror(int status);
 
 /* Validate a configuration without touching the device. */
 int epikv_check_cfg(const epikv_cfg* cfg);
+
+/* Bytes of one token's K or V row in the pool (the slot stride inside a
+ * page); 0 for an invalid cfg. */
+size_t epikv_kv_row_bytes(const epikv_cfg* cfg);
 
 /*
  * Scorer state carried from one call to the next (one flat device buffer,
@@ -519,6 +550,216 @@ int epikv_evict_step(const epikv_cfg* cfg, const epikv_step_io* io,
  */
 int epikv_evict_step_noalloc(const epikv_cfg* cfg, const epikv_step_io* io,
                              hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Filling and reading the cache
+ *
+ * These calls work on one layer of the pool.  `chunk` new tokens per
+ * sequence, as in the step; n_new (int32 [B], optional, NULL = chunk for
+ * every sequence) says how many of a sequence's chunk are real: tokens
+ * c < n_new[b], the rest is padding.  n_cached[b] counts the cached tokens
+ * with the new ones, so new token c of sequence b has slot
+ * n_cached[b] - n_new[b] + c.  A slot is a place in the cache, a position is
+ * the token's place in its text: an eviction lowers slots and leaves
+ * positions (the token ids the step carries in src_pos / dst_pos).
+ *
+ * seq_status (int32 [B], optional) is only raised here: a sequence with
+ * something out of range gets EPIKV_SEQ_RANGE, no call lowers a flag.
+ * Out of range are: n_new[b] outside [0, chunk], n_cached[b] outside
+ * [n_new[b], ld_pt*page_size] (the sequence counts as having no tokens), a
+ * page id outside [0, n_pages) (its tokens are neither written nor read, and
+ * attention leaves them out) and a position outside [0, n_pos) (the token is
+ * left out).
+ */
+
+/*
+ * A tensor [B][chunk][heads][head_dim] by its strides, in elements: element
+ * i of head h of token c of sequence b is at
+ *     base + b*ld_seq + c*ld_tok + h*ld_head + i.
+ * base 16-byte aligned, strides multiples of 8 and not negative (rows of one
+ * fused projection, [B][heads][chunk][head_dim] and broadcast inputs are all
+ * this).  Rows that are written must not overlap each other.
+ */
+typedef struct epikv_rows {
+  void* base;
+  int64_t ld_seq, ld_tok, ld_head;
+} epikv_rows;
+
+typedef enum epikv_dtype { EPIKV_DTYPE_BF16 = 0, EPIKV_DTYPE_FP32 = 1 } epikv_dtype;
+
+/* Which channels make pair i of the rotary_dim / 2 pairs. */
+typedef enum epikv_rope_layout {
+  EPIKV_ROPE_HALF = 0,        /* i and i + rotary_dim / 2 */
+  EPIKV_ROPE_INTERLEAVED = 1  /* 2i and 2i + 1 */
+} epikv_rope_layout;
+
+/* How the pairs' frequencies f_i = theta^(-2i / rotary_dim) are changed for
+ * contexts `factor` times as long as the `original` one of training. */
+typedef enum epikv_rope_scaling {
+  EPIKV_ROPE_PLAIN = 0,   /* f_i */
+  EPIKV_ROPE_LINEAR = 1,  /* f_i / factor */
+  EPIKV_ROPE_NTK = 2,     /* theta * factor^(r / (r - 2)) for theta, r = rotary_dim >= 4 */
+  EPIKV_ROPE_BANDS = 3,   /* mix by turns: with t_i = original*f_i / (2 pi) the
+                             turns over the original context and
+                             g = clamp((t_i - turns_low) / (turns_high - turns_low), 0, 1):
+                             g*f_i + (1 - g)*f_i / factor */
+  EPIKV_ROPE_YARN = 4     /* mix by pair: with i(t) = r/2 * ln(original / (2 pi t)) / ln(theta)
+                             the pair that makes t turns, lo = max(0, floor(i(turns_high))),
+                             hi = min(r - 1, ceil(i(turns_low))) (hi = lo + 0.001 if equal) and
+                             g = 1 - clamp((i - lo) / (hi - lo), 0, 1): as above */
+} epikv_rope_scaling;
+
+/* Rotary positions (host struct). */
+typedef struct epikv_rope_cfg {
+  int32_t rotary_dim;   /* r: channels rotated, the head's first; a multiple of 16 */
+  int32_t layout;       /* epikv_rope_layout */
+  int32_t scaling;      /* epikv_rope_scaling */
+  int32_t n_pos;        /* positions in the table, 1..2^24 */
+  int32_t original;     /* BANDS, YARN: original context, >= 1 */
+  float theta;          /* > 1 */
+  float factor;         /* > 0; ignored by PLAIN */
+  float turns_low, turns_high;  /* BANDS, YARN: 0 < low < high */
+  float amplitude;      /* multiplies every cosine and sine, > 0 (YaRN:
+                           0.1 ln(factor) + 1) */
+} epikv_rope_cfg;
+
+/* Fill *rope with r = 128, HALF, PLAIN, 32768 positions, original 8192,
+ * theta = 10000, factor = 1, turns 1 and 4, amplitude 1. */
+int epikv_default_rope(epikv_rope_cfg* rope);
+
+/* Validate without touching the device. */
+int epikv_check_rope(const epikv_rope_cfg* rope);
+
+/* Bytes of the table: float [n_pos][r / 2][2], the cosine and the sine of
+ * every pair's angle.  0 for an invalid rope. */
+size_t epikv_rope_table_bytes(const epikv_rope_cfg* rope);
+
+/* Fill the table (16-byte aligned device memory of the caller's), with
+ * angles, sines and cosines in 64 bits, rounded once. */
+int epikv_rope_table(const epikv_rope_cfg* rope, float* table, hipStream_t stream);
+
+/*
+ * epikv_rope -- rotate x [batch][chunk][n_heads][head_dim] into y.
+ *
+ * A pair (a, b) becomes (a cos - b sin, b cos + a sin) of its token's
+ * position; channels from rotary_dim on are copied.  Every product, sum and
+ * rounding is one of float32, the result is rounded once to the type.
+ * transpose != 0 takes -sin for sin: the gradient of the input from the
+ * gradient of the output (and, for amplitude 1, the inverse).
+ * head_dim a multiple of 16 from 16 to 1024, rotary_dim <= head_dim; dtype
+ * of x and y an epikv_dtype.  y may be x (same base and strides); any other
+ * overlap of the two is EPIKV_EALIAS.
+ * positions: int32, ld_pos = 0: [batch], the position of the sequence's
+ * first token, the rest follow; else [batch][ld_pos >= chunk], one a token.
+ * Tokens whose position is out of range are not written (and flagged).
+ */
+int epikv_rope(const epikv_rope_cfg* rope, const float* table, int32_t dtype,
+               int32_t batch, int32_t chunk, int32_t n_heads, int32_t head_dim,
+               const epikv_rows* x, const epikv_rows* y,
+               const int32_t* positions, int64_t ld_pos, int32_t transpose,
+               int32_t* seq_status, hipStream_t stream);
+
+/* Arguments of epikv_append (host struct; device pointers unless marked). */
+typedef struct epikv_append_io {
+  int32_t chunk;
+  int32_t layer;                /* [0, n_layers) */
+  epikv_pool pool;
+  const int32_t* page_table;    /* [B][ld_pt] */
+  int64_t ld_pt;
+  const int32_t* n_cached;      /* [B], with the new tokens */
+  const int32_t* n_new;         /* [B], optional */
+  epikv_rows k, v;              /* bf16 [B][chunk][n_kv_heads][head_dim] */
+  const epikv_rope_cfg* rope;   /* host; NULL: keys and queries as they are */
+  const float* rope_table;
+  const int32_t* positions;     /* as for epikv_rope; needed with rope or pos */
+  int64_t ld_pos;
+  int32_t n_heads;              /* query heads, used when q.base is given */
+  epikv_rows q, q_out;          /* optional: bf16 queries, rotated into q_out
+                                   (which may be q) in the same launch */
+  int32_t* pos;                 /* optional [B][ld_s]: pos[b][slot] = the
+                                   token's position, the ids the step moves */
+  int64_t ld_s;
+  int32_t* seq_status;          /* optional [B] */
+} epikv_append_io;
+
+/*
+ * epikv_append -- the new tokens' keys and values into the cache's pages,
+ * keys rotated on the way.
+ *
+ * Rotation as in epikv_rope; a bf16 cache rounds its result once, a 4-bit
+ * one quantises it unrounded.  A block's power of two is 2^e with
+ * e = floor(log2 m) - 2 for its largest magnitude m, one more when
+ * m > 7 * 2^e (there clipping to 6 would cost more than the coarser grid),
+ * -126 at least; its values round to the nearest code, ties to the even one.
+ * A block with a NaN or an infinity reads back as NaN.
+ * Queries of padding tokens (c >= n_new[b]) and of positions out of range are
+ * not written.  k and v must not overlap the pool (not checked).
+ * Pages of different sequences may be shared only where neither appends.
+ */
+int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io, hipStream_t stream);
+
+/* Arguments of epikv_read. */
+typedef struct epikv_read_io {
+  int32_t chunk;                /* slots read per sequence */
+  int32_t layer;
+  epikv_pool pool;
+  const int32_t* page_table;
+  int64_t ld_pt;
+  const int32_t* first;         /* [B]: the first slot read */
+  epikv_rows k, v;              /* out: bf16 [B][chunk][n_kv_heads][head_dim] */
+  int32_t* seq_status;          /* optional [B] */
+} epikv_read_io;
+
+/*
+ * epikv_read -- rows of the cache as bf16 values (what a 4-bit row stands
+ * for is exact in bf16 but for overflow to infinity): slots first[b] ...
+ * first[b] + chunk - 1.  Slots outside [0, ld_pt*page_size) or in pages out
+ * of range read as zeros, and flag the sequence.  k or v may have a NULL
+ * base (not read), not both.
+ */
+int epikv_read(const epikv_cfg* cfg, const epikv_read_io* io, hipStream_t stream);
+
+/* Arguments of epikv_attend. */
+typedef struct epikv_attend_io {
+  int32_t chunk;
+  int32_t layer;
+  epikv_pool pool;
+  const int32_t* page_table;
+  int64_t ld_pt;
+  const int32_t* n_cached;
+  const int32_t* n_new;         /* optional */
+  int32_t n_heads;              /* query heads, a multiple of n_kv_heads: query
+                                   head h reads KV head h*n_kv_heads/n_heads */
+  epikv_rows q;                 /* bf16 [B][chunk][n_heads][head_dim] */
+  epikv_rows out;               /* bf16, the same shape */
+  float* lse;                   /* optional [B][n_heads][chunk] */
+  float scale;                  /* of the scores; 0 = 1 / sqrt(head_dim) */
+  int32_t* seq_status;          /* optional [B] */
+  void* workspace;
+  size_t workspace_bytes;       /* >= epikv_attend_workspace_bytes(...) */
+} epikv_attend_io;
+
+/* Device scratch of epikv_attend (0: none needed, or invalid arguments). */
+size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads);
+
+/*
+ * epikv_attend -- attention of the new tokens' queries over the paged cache.
+ *
+ * Token c of sequence b sees slots j <= n_cached[b] - n_new[b] + c: its own,
+ * the new ones before it, and all older ones.
+ *   out[b][c][h] = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale*(q . k_j) - top)
+ *   lse[b][h][c] = top + log(sum_j w_j)
+ * Scores, sums and the product with V are kept in float32; the weights go
+ * into that product as bf16.  A token that sees nothing (padding, an empty
+ * or a flagged sequence, all its pages out of range, every score -infinity)
+ * has out 0 and lse -infinity.  Slots a token does not see, whatever they
+ * hold, do not reach its result.
+ * The cache is not written, so tokens must be appended before; out may not
+ * overlap q (EPIKV_EALIAS, checked on their whole spans).  The workspace
+ * (16-byte aligned, any contents) must overlap no other argument; calls that
+ * share one must not overlap in time.  May be captured in a HIP graph.
+ */
+int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io, hipStream_t stream);
 
 #ifdef __cplusplus
 }

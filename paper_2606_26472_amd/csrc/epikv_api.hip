@@ -12,14 +12,20 @@
 
 namespace epikv {
 
+bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
+
+// Bytes of one token's K or V row.
+int row_bytes(const epikv_cfg* c) {
+  const int hd = c->n_kv_heads * c->head_dim;
+  if (c->kv_format == EPIKV_KV_BF16) return hd * 2;
+  return std::max(128, (hd / 2 + hd / 32 + 15) / 16 * 16);
+}
 
 namespace {
 
 constexpr size_t kAlign = 256;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 int n_band(const epikv_cfg* c) { return c->n_band_a + c->n_band_b; }
 
@@ -34,8 +40,6 @@ bool uses_range(int signal) {
 int recent_of(const epikv_cfg* c) {
   return c->recent >= 0 ? c->recent : (c->budget / 4 < 128 ? c->budget / 4 : 128);
 }
-
-int row_bytes(const epikv_cfg* c) { return c->n_kv_heads * c->head_dim * 2; }
 
 int pages_for(int64_t tokens, int page_size) { return (int)((tokens + page_size - 1) / page_size); }
 
@@ -127,6 +131,8 @@ size_t partial_bytes(const epikv_cfg* c, int chunk) {
   return plane_sums_bytes(c, chunk) + prange_bytes(c, chunk);
 }
 
+}  // namespace
+
 int check_cfg(const epikv_cfg* c) {
   if (!c) return EPIKV_EINVAL_NULL;
   if (c->signal < EPIKV_SIGNAL_HS || c->signal > EPIKV_SIGNAL_LAGKV_KEY) return EPIKV_EINVAL_PARAM;
@@ -135,6 +141,8 @@ int check_cfg(const epikv_cfg* c) {
   if (c->window < 1 || c->window > EPIKV_MAX_WINDOW) return EPIKV_EINVAL_PARAM;
   if (!(c->eps >= 0.f) || !isfinite(c->eps)) return EPIKV_EINVAL_PARAM;
   if (c->budget < 1) return EPIKV_EINVAL_PARAM;
+  if (c->kv_format != EPIKV_KV_BF16 && c->kv_format != EPIKV_KV_MXFP4) return EPIKV_EINVAL_PARAM;
+  if (is_kv(c->signal) && c->kv_format != EPIKV_KV_BF16) return EPIKV_EINVAL_PARAM;
   if (c->recent < -1) return EPIKV_EINVAL_PARAM;
   if (c->batch < 1 || c->batch > 65535) return EPIKV_EINVAL_SHAPE;
   if (c->page_size < 1 || c->page_size > 1024) return EPIKV_EINVAL_SHAPE;
@@ -169,6 +177,8 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
 }
 
 int launched(hipError_t e) { return e == hipSuccess ? EPIKV_OK : EPIKV_ELAUNCH; }
+
+namespace {
 
 // ---------------------------------------------------------------------------
 // Per-stage validation + argument building
@@ -548,6 +558,7 @@ void inplace_slices(int64_t planes, int row_vec, int64_t cus, int32_t* n, int32_
     const int64_t blocks = planes * s;
     return (double)blocks / (double)((blocks + cus - 1) / cus * cus);
   };
+  take(1);  // (4-bit rows of no whole lines)
   for (int s = 1; planes * s <= cus && s <= row_vec; ++s)
     if (fits(s) && fill(s) >= 0.6) return take(s);
   const int cols = row_vec > 128 ? 128 : 32;
@@ -669,6 +680,7 @@ EPIKV_EXPORT int epikv_default_cfg(epikv_cfg* cfg) {
   cfg->budget = 4096;
   cfg->recent = -1;
   cfg->ema_alpha = 0.9f;
+  cfg->kv_format = EPIKV_KV_BF16;
   return EPIKV_OK;
 }
 
@@ -687,6 +699,10 @@ EPIKV_EXPORT const char* epikv_strerror(int status) {
 }
 
 EPIKV_EXPORT int epikv_check_cfg(const epikv_cfg* cfg) { return check_cfg(cfg); }
+
+EPIKV_EXPORT size_t epikv_kv_row_bytes(const epikv_cfg* cfg) {
+  return check_cfg(cfg) ? 0 : (size_t)row_bytes(cfg);
+}
 
 EPIKV_EXPORT size_t epikv_state_bytes(const epikv_cfg* cfg) {
   if (check_cfg(cfg)) return 0;

@@ -482,4 +482,83 @@ constexpr int kRedRowWords = 64 * 2 + 8 * 4;
 size_t lagkv_lds_bytes(int H, int d, bool lag, bool big);
 constexpr int kInplaceThreads = 1024;    // per-sequence check + score move
 
+// ---------------------------------------------------------------------------
+// Filling and reading the cache (one layer of the pool)
+// ---------------------------------------------------------------------------
+struct RowsArg {                           // epikv_rows, strides in elements
+  char* base;
+  int64_t ld_seq, ld_tok, ld_head;
+};
+
+struct RopeArg {
+  const float2* table;                     // [n_pos][r / 2] (cos, sin); nullptr: no rotation
+  const int32_t* positions;
+  int64_t ld_pos;
+  int32_t r, n_pos, interleaved, transpose;
+};
+
+// Where the tokens are: the layer's two planes, through the page table.
+struct PagedArgs {
+  char* plane[2];                          // K, V
+  int64_t s_page, n_pages;
+  const int32_t* pt;
+  int64_t ld_pt;
+  const int32_t* n_cached;
+  const int32_t* n_new;                    // or nullptr
+  int32_t* status;                         // or nullptr
+  int32_t B, C, H, d, page_size, page_shift, row_bytes;
+  int32_t max_tokens;                      // slots the page table covers
+};
+
+struct RopeTableArgs {
+  float* table;
+  int32_t n_pos, half, scaling, original;
+  double theta, factor, low, high, amplitude;
+};
+
+struct RopeArgs {
+  RowsArg x, y;
+  RopeArg rope;
+  int32_t B, C, heads, d;
+  int32_t fp32;
+  int32_t* status;
+};
+
+struct AppendArgs {
+  PagedArgs pg;
+  RopeArg rope;
+  RowsArg k, v, q, q_out;                  // q.base nullptr: none
+  int32_t heads;                           // query heads
+  int32_t* pos;
+  int64_t ld_s;
+};
+
+struct ReadArgs {
+  PagedArgs pg;                            // (n_cached: the first slots)
+  RowsArg k, v;
+};
+
+struct AttendArgs {
+  PagedArgs pg;
+  RowsArg q, out;
+  float* lse;
+  int32_t heads, G, R;                     // query heads; per KV head; rows C * G
+  float scale2;                            // scale * log2(e)
+};
+
+hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s);
+hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
+hipError_t launch_append(const AppendArgs& a, bool q4, hipStream_t s);
+hipError_t launch_read(const ReadArgs& a, bool q4, hipStream_t s);
+size_t attend_workspace(int B, int C, int H, int heads, int d, bool q4);
+hipError_t launch_attend(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
+
+// Shared host checks (epikv_api.hip).
+bool aligned16(const void* p);
+bool overlap(const void* a, size_t na, const void* b, size_t nb);
+int launched(hipError_t e);
+int row_bytes(const epikv_cfg* c);
+int check_cfg(const epikv_cfg* c);
+int check_pool(const epikv_pool* p);
+
 }  // namespace epikv

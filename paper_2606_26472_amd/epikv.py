@@ -42,6 +42,10 @@ SMOOTH_MEAN = 1
 SMOOTH_RAW = 2
 SMOOTH_EMA = 3
 MAX_BAND = 32
+KV_BF16, KV_MXFP4 = 0, 1
+DTYPE_BF16, DTYPE_FP32 = 0, 1
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4
 
 EXPORTED = ("epikv_default_cfg", "epikv_strerror", "epikv_check_cfg",
             "epikv_state_bytes", "epikv_state_layout",
@@ -50,7 +54,11 @@ EXPORTED = ("epikv_default_cfg", "epikv_strerror", "epikv_check_cfg",
             "epikv_zscore", "epikv_select", "epikv_select_workspace_bytes",
             "epikv_select_ws", "epikv_compact",
             "epikv_compact_inplace", "epikv_compact_remap",
-            "epikv_evict_step", "epikv_evict_step_noalloc")
+            "epikv_evict_step", "epikv_evict_step_noalloc",
+            "epikv_kv_row_bytes", "epikv_default_rope", "epikv_check_rope",
+            "epikv_rope_table_bytes", "epikv_rope_table", "epikv_rope",
+            "epikv_append", "epikv_read", "epikv_attend_workspace_bytes",
+            "epikv_attend")
 
 
 class EpikvError(RuntimeError):
@@ -67,7 +75,8 @@ class Cfg(ctypes.Structure):
                 ("window", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("signal", ctypes.c_int32), ("smoothing", ctypes.c_int32),
                 ("budget", ctypes.c_int32), ("recent", ctypes.c_int32),
-                ("ema_alpha", ctypes.c_float)]
+                ("ema_alpha", ctypes.c_float),
+                ("kv_format", ctypes.c_int32)]
 
 
 class Pool(ctypes.Structure):
@@ -96,6 +105,50 @@ class StepIO(ctypes.Structure):
                 ("in_place", ctypes.c_int32)]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("ld_seq", ctypes.c_int64),
+                ("ld_tok", ctypes.c_int64), ("ld_head", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("n_pos", ctypes.c_int32),
+                ("original", ctypes.c_int32), ("theta", ctypes.c_float),
+                ("factor", ctypes.c_float), ("turns_low", ctypes.c_float),
+                ("turns_high", ctypes.c_float), ("amplitude", ctypes.c_float)]
+
+
+class AppendIO(ctypes.Structure):
+    _fields_ = [("chunk", ctypes.c_int32), ("layer", ctypes.c_int32),
+                ("pool", Pool), ("page_table", ctypes.c_void_p),
+                ("ld_pt", ctypes.c_int64), ("n_cached", ctypes.c_void_p),
+                ("n_new", ctypes.c_void_p), ("k", Rows), ("v", Rows),
+                ("rope", ctypes.POINTER(Rope)),
+                ("rope_table", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("ld_pos", ctypes.c_int64),
+                ("n_heads", ctypes.c_int32), ("q", Rows), ("q_out", Rows),
+                ("pos", ctypes.c_void_p), ("ld_s", ctypes.c_int64),
+                ("seq_status", ctypes.c_void_p)]
+
+
+class ReadIO(ctypes.Structure):
+    _fields_ = [("chunk", ctypes.c_int32), ("layer", ctypes.c_int32),
+                ("pool", Pool), ("page_table", ctypes.c_void_p),
+                ("ld_pt", ctypes.c_int64), ("first", ctypes.c_void_p),
+                ("k", Rows), ("v", Rows), ("seq_status", ctypes.c_void_p)]
+
+
+class AttendIO(ctypes.Structure):
+    _fields_ = [("chunk", ctypes.c_int32), ("layer", ctypes.c_int32),
+                ("pool", Pool), ("page_table", ctypes.c_void_p),
+                ("ld_pt", ctypes.c_int64), ("n_cached", ctypes.c_void_p),
+                ("n_new", ctypes.c_void_p), ("n_heads", ctypes.c_int32),
+                ("q", Rows), ("out", Rows), ("lse", ctypes.c_void_p),
+                ("scale", ctypes.c_float), ("seq_status", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -122,6 +175,7 @@ def lib() -> ctypes.CDLL:
     i32, i64, sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     cfgp = ctypes.POINTER(Cfg)
     poolp = ctypes.POINTER(Pool)
+    ropep, rowsp = ctypes.POINTER(Rope), ctypes.POINTER(Rows)
     sig = {
         "epikv_default_cfg": (ctypes.c_int, [cfgp]),
         "epikv_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -149,6 +203,17 @@ def lib() -> ctypes.CDLL:
         "epikv_evict_step": (ctypes.c_int, [cfgp, ctypes.POINTER(StepIO), P]),
         "epikv_evict_step_noalloc": (ctypes.c_int,
                                      [cfgp, ctypes.POINTER(StepIO), P]),
+        "epikv_kv_row_bytes": (sz, [cfgp]),
+        "epikv_default_rope": (ctypes.c_int, [ropep]),
+        "epikv_check_rope": (ctypes.c_int, [ropep]),
+        "epikv_rope_table_bytes": (sz, [ropep]),
+        "epikv_rope_table": (ctypes.c_int, [ropep, P, P]),
+        "epikv_rope": (ctypes.c_int, [ropep, P, i32, i32, i32, i32, i32, rowsp,
+                                      rowsp, P, i64, i32, P, P]),
+        "epikv_append": (ctypes.c_int, [cfgp, ctypes.POINTER(AppendIO), P]),
+        "epikv_read": (ctypes.c_int, [cfgp, ctypes.POINTER(ReadIO), P]),
+        "epikv_attend_workspace_bytes": (sz, [cfgp, i32, i32]),
+        "epikv_attend": (ctypes.c_int, [cfgp, ctypes.POINTER(AttendIO), P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -241,8 +306,47 @@ def select_workspace_bytes(cfg: Cfg) -> int:
     return int(lib().epikv_select_workspace_bytes(ctypes.byref(cfg)))
 
 
+def kv_row_bytes(cfg: Cfg) -> int:
+    return int(lib().epikv_kv_row_bytes(ctypes.byref(cfg)))
+
+
+def attend_workspace_bytes(cfg: Cfg, chunk: int, n_heads: int) -> int:
+    return int(lib().epikv_attend_workspace_bytes(ctypes.byref(cfg), int(chunk),
+                                                  int(n_heads)))
+
+
+def default_rope(**overrides) -> Rope:
+    r = Rope()
+    _check(lib().epikv_default_rope(ctypes.byref(r)), "epikv_default_rope")
+    for k, v in overrides.items():
+        setattr(r, k, v)
+    return r
+
+
+def check_rope(rope: Rope) -> int:
+    return lib().epikv_check_rope(ctypes.byref(rope))
+
+
+def rope_table_bytes(rope: Rope) -> int:
+    return int(lib().epikv_rope_table_bytes(ctypes.byref(rope)))
+
+
+def rows_of(t) -> Rows:
+    """epikv_rows describing a [B][chunk][heads][head_dim] tensor (any
+    strides, channels adjacent); None gives a NULL base."""
+    if t is None:
+        return Rows(None, 0, 0, 0)
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError("rows need a [batch][chunk][heads][head_dim] tensor "
+                         "with adjacent channels")
+    # (the stride of an axis of one entry means nothing)
+    s = [t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)]
+    return Rows(t.data_ptr(), s[0], s[1], s[2])
+
+
 def pool_of(t) -> Pool:
-    """epikv_pool describing a tensor laid out [L][2][n_pages][page][H][d]."""
+    """epikv_pool describing a tensor laid out [L][2][n_pages][page][H][d]
+    (4-bit rows: uint8 [L][2][n_pages][page][row_bytes])."""
     es = t.element_size()
     L, two, n_pages = t.shape[0], t.shape[1], t.shape[2]
     assert two == 2
@@ -406,6 +510,143 @@ def epikv_evict_step_noalloc(cfg: Cfg, io: StepIO, stream=None):
     _check(lib().epikv_evict_step_noalloc(ctypes.byref(cfg), ctypes.byref(io),
                                           _stream(stream)),
            "epikv_evict_step_noalloc")
+
+
+# ---------------------------------------------------------------------------
+# Filling and reading the cache
+# ---------------------------------------------------------------------------
+def _expect(t, dtype, shape, what):
+    """A wrong type or shape would be read or written past its end."""
+    if t is None or isinstance(t, Rows):
+        return
+    import torch
+    want = getattr(torch, dtype)
+    if t.dtype not in (want, torch.int16 if dtype == "bfloat16" else want):
+        raise ValueError(f"{what}: {dtype} expected, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
+
+
+def _same_shape(cfg: Cfg, io, where):
+    if io._dims != (cfg.batch, cfg.n_kv_heads, cfg.head_dim):
+        raise ValueError(f"{where}: built for (batch, n_kv_heads, head_dim) = {io._dims}, "
+                         f"cfg has {(cfg.batch, cfg.n_kv_heads, cfg.head_dim)}")
+
+
+def _as_rows(t) -> Rows:
+    return t if isinstance(t, Rows) else rows_of(t)
+
+
+def epikv_rope_table(rope: Rope, table, stream=None):
+    if not isinstance(table, int):
+        have = table.numel() * table.element_size()
+        if have < rope_table_bytes(rope):
+            raise ValueError(f"table holds {have} bytes, {rope_table_bytes(rope)} needed")
+    _check(lib().epikv_rope_table(ctypes.byref(rope), _ptr(table), _stream(stream)),
+           "epikv_rope_table")
+
+
+def epikv_rope(rope: Rope, table, dtype, batch, chunk, n_heads, head_dim, x,
+               y, positions, ld_pos=0, transpose=False, seq_status=None,
+               stream=None):
+    """x and y: tensors [batch][chunk][n_heads][head_dim], or Rows."""
+    xr, yr = _as_rows(x), _as_rows(y)
+    for t, what in ((x, "x"), (y, "y")):
+        _expect(t, "float32" if dtype == DTYPE_FP32 else "bfloat16",
+                (batch, chunk, n_heads, head_dim), what)
+    _check(lib().epikv_rope(
+        ctypes.byref(rope), _ptr(table), int(dtype), int(batch), int(chunk),
+        int(n_heads), int(head_dim), ctypes.byref(xr), ctypes.byref(yr),
+        _ptr(positions), int(ld_pos), int(transpose), _ptr(seq_status),
+        _stream(stream)), "epikv_rope")
+
+
+def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
+                   n_new=None, rope: Rope | None = None, table=None,
+                   positions=None, ld_pos=0, q=None, q_out=None, pos=None,
+                   ld_s=0, seq_status=None) -> AppendIO:
+    """Build the epikv_append_io struct; k, v, q and q_out are tensors
+    [B][chunk][heads][head_dim].  The object keeps what it was built from."""
+    for t, like, what in ((v, k, "v"), (q_out, q, "q_out")):
+        if t is not None:
+            _expect(t, "bfloat16", like.shape, what)
+    _expect(k, "bfloat16", (k.shape[0], int(chunk)) + tuple(k.shape[2:]), "k")
+    if q is not None:
+        _expect(q, "bfloat16", (k.shape[0], int(chunk), q.shape[2], k.shape[3]), "q")
+    io = AppendIO()
+    io._dims = (k.shape[0], k.shape[2], k.shape[3])
+    io._keepalive = [page_table, n_cached, n_new, k, v, rope, table, positions,
+                     q, q_out, pos, seq_status]
+    io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
+    io.page_table, io.ld_pt = _ptr(page_table), int(ld_pt)
+    io.n_cached, io.n_new = _ptr(n_cached), _ptr(n_new)
+    io.k, io.v = rows_of(k), rows_of(v)
+    io.rope = ctypes.pointer(rope) if rope is not None else None
+    io.rope_table = _ptr(table)
+    io.positions, io.ld_pos = _ptr(positions), int(ld_pos)
+    io.n_heads = int(q.shape[2]) if q is not None else 0
+    io.q, io.q_out = rows_of(q), rows_of(q_out)
+    io.pos, io.ld_s, io.seq_status = _ptr(pos), int(ld_s), _ptr(seq_status)
+    return io
+
+
+def epikv_append(cfg: Cfg, io: AppendIO, stream=None):
+    _same_shape(cfg, io, "epikv_append")
+    _check(lib().epikv_append(ctypes.byref(cfg), ctypes.byref(io),
+                              _stream(stream)), "epikv_append")
+
+
+def make_read_io(chunk, pool: Pool, layer, page_table, ld_pt, first, k=None,
+                 v=None, seq_status=None) -> ReadIO:
+    like = v if k is None else k
+    for t, what in ((k, "k"), (v, "v")):
+        _expect(t, "bfloat16", (like.shape[0], int(chunk)) + tuple(like.shape[2:]), what)
+    io = ReadIO()
+    io._dims = (like.shape[0], like.shape[2], like.shape[3])
+    io._keepalive = [page_table, first, k, v, seq_status]
+    io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
+    io.page_table, io.ld_pt, io.first = _ptr(page_table), int(ld_pt), _ptr(first)
+    io.k, io.v, io.seq_status = rows_of(k), rows_of(v), _ptr(seq_status)
+    return io
+
+
+def epikv_read(cfg: Cfg, io: ReadIO, stream=None):
+    _same_shape(cfg, io, "epikv_read")
+    _check(lib().epikv_read(ctypes.byref(cfg), ctypes.byref(io),
+                            _stream(stream)), "epikv_read")
+
+
+def make_attend_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, q, out,
+                   n_new=None, lse=None, scale=0.0, seq_status=None,
+                   workspace=None, workspace_bytes_=0) -> AttendIO:
+    """Build the epikv_attend_io struct; q and out are tensors
+    [B][chunk][n_heads][head_dim], lse float32 [B][n_heads][chunk]."""
+    B, _, n_heads, d = q.shape
+    for t, what in ((q, "q"), (out, "out")):
+        _expect(t, "bfloat16", (B, int(chunk), n_heads, d), what)
+    if lse is not None:
+        _expect(lse, "float32", (B, n_heads, int(chunk)), "lse")
+        if not lse.is_contiguous():
+            raise ValueError("lse must be contiguous")
+    io = AttendIO()
+    io._dims = (B, d)
+    io._keepalive = [page_table, n_cached, n_new, q, out, lse, seq_status, workspace]
+    io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
+    io.page_table, io.ld_pt = _ptr(page_table), int(ld_pt)
+    io.n_cached, io.n_new, io.n_heads = _ptr(n_cached), _ptr(n_new), int(n_heads)
+    io.q, io.out, io.lse = rows_of(q), rows_of(out), _ptr(lse)
+    io.scale, io.seq_status = float(scale), _ptr(seq_status)
+    io.workspace = _ws(workspace, workspace_bytes_)
+    io.workspace_bytes = int(workspace_bytes_)
+    return io
+
+
+def epikv_attend(cfg: Cfg, io: AttendIO, stream=None):
+    if io._dims != (cfg.batch, cfg.head_dim):
+        raise ValueError(f"epikv_attend: built for (batch, head_dim) = {io._dims}, "
+                         f"cfg has {(cfg.batch, cfg.head_dim)}")
+    _check(lib().epikv_attend(ctypes.byref(cfg), ctypes.byref(io),
+                              _stream(stream)), "epikv_attend")
 
 
 # ---------------------------------------------------------------------------
