@@ -3,7 +3,7 @@
 // out = sum_j w_j v_j / sum_j w_j with w_j = exp(scale * (q . k_j) - top), in
 // one pass over the rows: the running maximum `top` and the sums made with
 // it are rescaled when it grows.
-#include "cache_impl.h"
+#include "attend_impl.h"
 
 namespace epikv {
 namespace {
@@ -97,9 +97,13 @@ hipError_t launch_plain(const AttendArgs& a, bool q4, hipStream_t s) {
 
 }  // namespace
 
-size_t attend_workspace(int, int, int, int, int, bool) { return 0; }
+size_t attend_workspace(int B, int C, int H, int heads, int d, bool) {
+  const int R = C * (heads / H);
+  return attend_wave_tiles(R) ? attend_wave_workspace(B, H, R, d) : 0;
+}
 
-hipError_t launch_attend(const AttendArgs& a, bool q4, void*, hipStream_t s) {
+hipError_t launch_attend(const AttendArgs& a, bool q4, void* ws, hipStream_t s) {
+  if (attend_wave_tiles(a.R)) return launch_attend_wave(a, q4, ws, s);
   if (a.pg.d == 64) return launch_plain<64>(a, q4, s);
   if (a.pg.d == 128) return launch_plain<128>(a, q4, s);
   return launch_plain<256>(a, q4, s);

@@ -1,0 +1,86 @@
+// What the attention kernels share: how the tokens are cut into shares, the
+// running softmax, and matrix-core fragments.
+#pragma once
+
+#include "cache_impl.h"
+
+namespace epikv {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLn2 = 0.69314718055994531f;
+constexpr float kNegInf = -__builtin_inff();
+
+// Tokens of one step of a wavefront's walk along a sequence, the unit that
+// shares are counted in.
+constexpr int kUnit = 32;
+
+// One sequence's units are cut over several teams of wavefronts when the
+// batch is small: all sequences' units in a row, cut into even shares of at
+// least kMinUnits, so that ragged lengths cost no balance.  A team's share may
+// span sequences; its part of sequence b goes to partial slot team + b, which
+// no other (team, sequence) pair of the staircase has.
+struct WavePlan {
+  int32_t n_teams;  // shares (split) or sequences
+  int32_t hw;       // KV heads a team walks side by side, a wavefront each
+  int32_t tpw;      // teams per workgroup
+  int32_t split;    // sequences are cut
+  float* part_o;    // [n_teams + B][H][R][d] unnormalised
+  float2* part_ml;  // [n_teams + B][H][R] maximum (base 2) and sum
+};
+constexpr int kSplitBatch = 256;  // largest batch whose sequences are cut
+constexpr int kMinUnits = 2;
+
+__device__ __forceinline__ int units_of(const SeqTokens& t) {
+  return t.nn > 0 ? (t.n + kUnit - 1) / kUnit : 0;
+}
+
+// Inclusive sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const int o = __shfl_up(v, m);
+    if (lane >= m) v += o;
+  }
+  return v;
+}
+
+// Units of all sequences (at most 2^23 each, so int32 holds their sum).
+__device__ __forceinline__ int total_units(const PagedArgs& g, int lane) {
+  int sum = 0;
+  for (int b = lane; b < g.B; b += 64) sum += units_of(seq_tokens(g, b));
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+  return sum;
+}
+
+__device__ __forceinline__ int units_per_team(int total, int n_teams) {
+  return max(kMinUnits, (total + n_teams - 1) / n_teams);
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+__device__ __forceinline__ bf16x8 as_bf16x8(u32x4 w) { return __builtin_bit_cast(bf16x8, w); }
+
+// Whether one of a word's two bf16 halves is a NaN or an infinity.
+__device__ __forceinline__ bool word_not_finite(uint32_t w) {
+  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
+}
+
+// Lower / upper halves of two words.
+__device__ __forceinline__ uint32_t halves_lo(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+__device__ __forceinline__ uint32_t halves_hi(uint32_t lo, uint32_t hi) {
+  return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+int attend_wave_tiles(int R);  // 16-row tiles of the wavefront kernel, 0: too many rows
+size_t attend_wave_workspace(int B, int H, int R, int d);
+hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
+
+}  // namespace epikv

@@ -1,0 +1,583 @@
+// Attention for few query rows per KV head (single tokens, short chunks): a
+// wavefront per (KV head, share of a sequence), which walks the rows once,
+// straight from memory into matrix-core operands.
+//
+// Scores are made transposed, S^T = K Q^T, so that a step's weights are
+// already laid out as the second operand of O^T = V^T P^T: with v_mfma
+// 16x16x32, lane (n, g) = (lane % 16, lane / 16) gets the scores of query row
+// n against tokens 4g .. 4g+3 of each 16-token tile, and 32 tokens make its 8
+// values of the second product.  Nothing passes through LDS but row addresses,
+// and the running maximum's growth is the only exchange between lanes.
+#include "attend_impl.h"
+
+namespace epikv {
+namespace {
+
+template <int D, bool Q4>
+struct Step {  // 32 tokens on their way from memory
+  static constexpr int KS = D / 32;   // first product: 32 channels an instruction
+  static constexpr int VC = D / 16;   // second product: channels a lane brings, instructions
+  static constexpr int KW = Q4 ? KS : KS * 4;      // words per 16-token tile
+  static constexpr int VW = Q4 ? (VC + 7) / 8 : VC / 2;  // words per token
+  uint32_t k[2][KW];
+  uint32_t v[8][VW];
+  uint32_t ks[2], vs[8];  // 4-bit rows: scale bytes
+};
+
+template <int D, bool Q4>
+__device__ __forceinline__ void load_k(Step<D, Q4>& st, const AttendArgs& a, const int64_t* off, int h,
+                                       int n, int g) {
+  using S = Step<D, Q4>;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const char* row = a.pg.plane[0] + off[16 * t + n];
+    if constexpr (Q4) {
+      const char* p = row + h * (D / 2) + g * (D / 8);
+      if constexpr (D == 64) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+        st.k[t][0] = w[0];
+        st.k[t][1] = w[1];
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::KW / 4; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(p + 16 * i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) st.k[t][4 * i + j] = w[j];
+        }
+      }
+      const uint8_t* sc = reinterpret_cast<const uint8_t*>(row) + a.pg.H * (D / 2) + h * (D / 32);
+      if constexpr (D == 64) st.ks[t] = sc[g / 2];
+      if constexpr (D == 128) st.ks[t] = sc[g];
+      if constexpr (D == 256) st.ks[t] = *reinterpret_cast<const uint16_t*>(sc + 2 * g);
+    } else {
+      const char* p = row + h * (D * 2) + g * 16;
+#pragma unroll
+      for (int i = 0; i < S::KS; ++i) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(p + 64 * i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st.k[t][4 * i + j] = w[j];
+      }
+    }
+  }
+}
+
+template <int D, bool Q4>
+__device__ __forceinline__ void load_v(Step<D, Q4>& st, const AttendArgs& a, const int64_t* off, int h,
+                                       int n, int g) {
+  using S = Step<D, Q4>;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const char* row = a.pg.plane[1] + off[(e < 4 ? 0 : 12) + 4 * g + e];
+    if constexpr (Q4) {
+      const char* p = row + h * (D / 2) + n * (S::VC / 2);
+      if constexpr (D == 64) st.v[e][0] = *reinterpret_cast<const uint16_t*>(p);
+      if constexpr (D == 128) st.v[e][0] = *reinterpret_cast<const uint32_t*>(p);
+      if constexpr (D == 256) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+        st.v[e][0] = w[0];
+        st.v[e][1] = w[1];
+      }
+      st.vs[e] = reinterpret_cast<const uint8_t*>(row)[a.pg.H * (D / 2) + h * (D / 32) + n * S::VC / 32];
+    } else {
+      const char* p = row + h * (D * 2) + n * (S::VC * 2);
+      if constexpr (D == 64) {
+        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+        st.v[e][0] = w[0];
+        st.v[e][1] = w[1];
+      } else {
+#pragma unroll
+        for (int i = 0; i < S::VW / 4; ++i) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(p + 16 * i);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) st.v[e][4 * i + j] = w[j];
+        }
+      }
+    }
+  }
+}
+
+// Word w (two channels) of the values that a lane holds of token e.
+template <int D, bool Q4>
+__device__ __forceinline__ uint32_t v_word(const Step<D, Q4>& st, int e, int w) {
+  if constexpr (!Q4) return st.v[e][w];
+  const uint32_t codes = st.v[e][w / 4];
+  const float s = block_scale(st.vs[e]);
+  switch (w % 4) {
+    case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
+    case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
+    case 2: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2));
+    default: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3));
+  }
+}
+
+// Units [u0, u1) of sequence b for KV head h.  `off`: this wavefront's two
+// tables of row offsets.  whole: the units are all of the sequence's, the
+// result is final; else it goes to partial slot `slot`.
+template <int D, int NT, bool Q4>
+__device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
+                             int u0, int u1, bool whole, int slot, int64_t (*off)[kUnit], int lane) {
+  using S = Step<D, Q4>;
+  constexpr int KS = S::KS, VC = S::VC;
+  const PagedArgs& g = a.pg;
+  const int n = lane & 15, q4 = lane >> 4;
+  const int rows = tk.nn * a.G;  // rows of real tokens
+  bf16x8 qf[NT][KS];
+  f32x4 o[NT][VC];
+  float top[NT], sum[NT];
+  int lim[NT];  // slots this lane's row sees
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int r = t * 16 + n;
+    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+    const bool real = r < rows;
+    const char* qp = a.q.base + (b * a.q.ld_seq + c * a.q.ld_tok + hq * a.q.ld_head) * 2;
+    lim[t] = real ? tk.n - tk.nn + c + 1 : 0;
+    top[t] = kNegInf;
+    sum[t] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int ch = Q4 ? (D / 4) * q4 + 8 * s : 32 * s + 8 * q4;
+      u32x4 w = {0, 0, 0, 0};
+      if (real) w = *reinterpret_cast<const u32x4*>(qp + ch * 2);
+      qf[t][s] = as_bf16x8(w);
+    }
+#pragma unroll
+    for (int j = 0; j < VC; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int begin = u0 * kUnit, end = min(tk.n, u1 * kUnit);  // this share's slots (end > begin)
+  const int seen_by_all = tk.n - tk.nn + 1;
+  const int32_t* pt = g.pt + (int64_t)b * g.ld_pt;
+  // The page entry of the token this lane stands for in a step (past the
+  // share's end: the last one's, whose row costs no more memory traffic).
+  auto page_index = [&](int tok) {
+    return g.page_shift >= 0 ? tok >> g.page_shift : (int)((uint32_t)tok / (uint32_t)g.page_size);
+  };
+  const int at32 = lane & (kUnit - 1);
+  auto load_entry = [&](int base) { return pt[page_index(min(base + at32, end - 1))]; };
+  bool any_bad = false;
+  // The step's row offsets to LDS; returns which of its tokens exist.
+  auto put_offsets = [&](int base, int pg, int64_t* table) -> uint32_t {
+    const int tok = min(base + at32, end - 1);
+    const bool good = pg >= 0 && pg < g.n_pages;
+    const int64_t at = (int64_t)pg * g.s_page + (int64_t)(tok - page_index(tok) * g.page_size) * g.row_bytes;
+    wave_sync();
+    table[at32] = good ? at : 0;
+    wave_sync();
+    any_bad |= !good;
+    return (uint32_t)__ballot(good && base + at32 < end);
+  };
+
+  Step<D, Q4> st;
+  int entry = load_entry(begin);
+  uint32_t ok = put_offsets(begin, entry, off[0]);
+  entry = load_entry(begin + kUnit);
+  load_k<D, Q4>(st, a, off[0], h, n, q4);
+  load_v<D, Q4>(st, a, off[0], h, n, q4);
+  int buf = 0;
+  // A step takes 32 tokens; the next one's keys are on their way once this
+  // one's are used up, and so its values.
+#pragma clang loop unroll(disable)
+  for (int base = begin; base < end; base += kUnit) {
+    buf ^= 1;
+    const uint32_t ok_next = put_offsets(base + kUnit, entry, off[buf]);
+    entry = load_entry(base + 2 * kUnit);
+    f32x4 s[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        u32x4 w;
+        if constexpr (Q4) {
+          const uint32_t byte = D == 256 ? (k < KS / 2 ? st.ks[i] & 255u : st.ks[i] >> 8) : st.ks[i];
+          w = decode8(st.k[i][k], block_scale(byte));
+        } else {
+          w = u32x4{st.k[i][4 * k], st.k[i][4 * k + 1], st.k[i][4 * k + 2], st.k[i][4 * k + 3]};
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) s[t][i] = mfma16(as_bf16x8(w), qf[t][k], s[t][i]);
+      }
+    load_k<D, Q4>(st, a, off[buf], h, n, q4);
+    const bool special = ok != 0xffffffffu || base + 32 > seen_by_all;
+    bf16x8 pf[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = s[t][e / 4][e % 4];
+      if (special) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int j = (e < 4 ? 0 : 12) + 4 * q4 + e;
+          x[e] = (ok >> j & 1u) && base + j < lim[t] ? x[e] : kNegInf;
+        }
+      }
+      float m = x[0];
+#pragma unroll
+      for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
+      m *= a.scale2;
+      // The maximum may lag by 2^8: weights up to 256 lose nothing, and most
+      // steps then exchange and rescale nothing.
+      if (__any(m > top[t] + 8.f)) {
+        m = fmaxf(m, __shfl_xor(m, 16));
+        m = fmaxf(m, __shfl_xor(m, 32));
+        const float grown = fmaxf(top[t], m);
+        const float f = grown == top[t] ? 1.f : exp2_fast(top[t] - grown);
+        top[t] = grown;
+        sum[t] *= f;
+#pragma unroll
+        for (int j = 0; j < VC; ++j) o[t][j] *= f;
+      }
+      const float base2 = top[t] == kNegInf ? 0.f : top[t];
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[e] = exp2_fast(fmaf(x[e], a.scale2, -base2));
+        sum[t] += w[e];
+      }
+      pf[t] = as_bf16x8(u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]),
+                              pack_bf16(w[6], w[7])});
+    }
+    // V: a lane holds 8 tokens of VC channels; an instruction takes one
+    // channel's 8 tokens, two channels come of 8 words.
+    if (!special) {
+#pragma unroll
+      for (int w = 0; w < VC / 2; ++w) {
+        u32x4 c0, c1;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+          c0[i] = halves_lo(x, y);
+          c1[i] = halves_hi(x, y);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          o[t][2 * w] = mfma16(as_bf16x8(c0), pf[t], o[t][2 * w]);
+          o[t][2 * w + 1] = mfma16(as_bf16x8(c1), pf[t], o[t][2 * w + 1]);
+        }
+      }
+    } else {
+      // What does not exist counts as 0, whatever its bytes are.  A NaN or an
+      // infinity that some rows see and others do not (0 times it is NaN)
+      // needs a pass for each token c, without the values hidden from it.
+      auto masks = [&](int seen) {
+        u32x4 m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = (i < 2 ? 0 : 12) + 4 * q4 + 2 * i;
+          m[i] = ((ok >> j & 1u) && base + j < seen ? 0xffffu : 0u) |
+                 ((ok >> (j + 1) & 1u) && base + j + 1 < seen ? 0xffff0000u : 0u);
+        }
+        return m;
+      };
+      const u32x4 there = masks(tk.n);
+      bool odd = false;
+      if (tk.nn > 1) {
+#pragma unroll
+        for (int w = 0; w < VC / 2; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+            odd |= word_not_finite(halves_lo(x, y) & there[i]) | word_not_finite(halves_hi(x, y) & there[i]);
+          }
+      }
+      const bool by_token = __any(odd);
+      for (int c = by_token ? 0 : tk.nn - 1; c < tk.nn; ++c) {
+        const int seen = tk.n - tk.nn + c + 1;
+        const u32x4 m = masks(seen);
+        // (what a pass makes of the values is made anew: kept for the next
+        // one it would take a register file of its own)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int w = 0; w < S::VW; ++w) asm volatile("" : "+v"(st.v[e][w]));
+#pragma unroll
+        for (int w = 0; w < VC / 2; ++w) {
+          u32x4 c0, c1;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+            c0[i] = halves_lo(x, y) & m[i];
+            c1[i] = halves_hi(x, y) & m[i];
+          }
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            const f32x4 y0 = mfma16(as_bf16x8(c0), pf[t], o[t][2 * w]);
+            const f32x4 y1 = mfma16(as_bf16x8(c1), pf[t], o[t][2 * w + 1]);
+            if (!by_token || lim[t] == seen) {
+              o[t][2 * w] = y0;
+              o[t][2 * w + 1] = y1;
+            }
+          }
+        }
+      }
+    }
+    load_v<D, Q4>(st, a, off[buf], h, n, q4);
+    ok = ok_next;
+  }
+  if (__any(any_bad) && lane == 0) raise_flag(g.status, b);
+
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    sum[t] += __shfl_xor(sum[t], 16);
+    sum[t] += __shfl_xor(sum[t], 32);
+    const int r = t * 16 + n;
+    if (r >= a.R) continue;
+    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+    const bool real = r < rows;
+    // (lane (n, q4) holds channels D/4*q4 + VC*i + j of row r)
+    if (whole) {
+      const bool some = real && sum[t] != 0.f;
+      const float inv = 1.f / sum[t];
+      char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head + (D / 4) * q4) * 2;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < VC; j += 4) {
+          u32x2 w = {0u, 0u};
+          if (some) {
+            w[0] = pack_bf16(o[t][j][i] * inv, o[t][j + 1][i] * inv);
+            w[1] = pack_bf16(o[t][j + 2][i] * inv, o[t][j + 3][i] * inv);
+          }
+          *reinterpret_cast<u32x2*>(op + (VC * i + j) * 2) = w;
+        }
+      if (a.lse && q4 == 0)
+        a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
+            some ? (top[t] + __builtin_amdgcn_logf(sum[t])) * kLn2 : kNegInf;
+    } else if (real) {
+      const int64_t at = ((int64_t)slot * g.H + h) * a.R + r;
+      float* po = p.part_o + at * D + (D / 4) * q4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < VC; j += 4)
+          *reinterpret_cast<f32x4*>(po + VC * i + j) =
+              f32x4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
+      if (q4 == 0) p.part_ml[at] = make_float2(top[t], sum[t]);
+    }
+  }
+}
+
+// The outputs of a sequence with nothing to see.
+template <int D>
+__device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
+  for (int i = lane; i < a.R * (D / 8); i += 64) {
+    const int r = i / (D / 8), x = i - r * (D / 8);
+    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+    *reinterpret_cast<u32x4*>(a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head + x * 8) * 2) =
+        u32x4{0, 0, 0, 0};
+    if (a.lse && x == 0) a.lse[((int64_t)b * a.heads + hq) * a.pg.C + c] = kNegInf;
+  }
+}
+
+template <int D, int NT, bool Q4>
+__global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
+  __shared__ __align__(16) int64_t s_off[8][2][kUnit];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const PagedArgs& g = a.pg;
+  const int h = blockIdx.y * p.hw + wave % p.hw;
+  const int64_t team = linear_block() * p.tpw + wave / p.hw;
+  if (h >= g.H || team >= p.n_teams) return;  // (no workgroup barrier below)
+  if (!p.split) {
+    const int b = (int)team;
+    const SeqTokens t = seq_tokens(g, b);
+    if (t.bad && lane == 0) raise_flag(g.status, b);
+    const int u = units_of(t);
+    if (u == 0)
+      attend_nothing<D>(a, b, h, lane);
+    else
+      attend_share<D, NT, Q4>(a, p, b, h, t, 0, u, true, 0, s_off[wave], lane);
+    return;
+  }
+  const int total = total_units(g, lane);
+  const int per = units_per_team(total, p.n_teams);
+  int lo = (int)team * per;
+  const int hi = min(total, lo + per);
+  if (lo >= hi) return;
+  // the sequence that holds unit lo, and the units before it
+  int b0 = 0, before = 0;
+  for (;; b0 += 64) {
+    const int b = b0 + lane;
+    const int u = b < g.B ? units_of(seq_tokens(g, b)) : 0;
+    const int upto = before + wave_scan(u, lane);
+    const uint64_t past = __ballot(upto > lo);
+    if (past) {
+      const int k = __ffsll((unsigned long long)past) - 1;
+      before = __builtin_amdgcn_readlane(upto - u, k);
+      b0 += k;
+      break;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  for (int b = __builtin_amdgcn_readfirstlane(b0); lo < hi; ++b) {
+    const SeqTokens t = seq_tokens(g, b);
+    const int u = units_of(t);
+    if (u == 0) continue;
+    const int u0 = lo - before, u1 = min(u, hi - before);
+    attend_share<D, NT, Q4>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_off[wave], lane);
+    lo = before + u1;
+    before += u;
+  }
+}
+
+// Joins the shares of one row: a workgroup per (sequence, query row), its
+// wavefronts taking turns over the shares, in a fixed order.
+constexpr int kJoinShares = 2048;  // (teams are fewer)
+
+template <int D>
+__global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) {
+  constexpr int E = D / 64;
+  __shared__ float s_w[kJoinShares];
+  __shared__ float s_o[16][D];
+  __shared__ float s_sum[16];
+  const PagedArgs& g = a.pg;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int64_t id = linear_block();
+  const int per_seq = a.R * g.H;
+  const int b = (int)(id / per_seq);
+  if (b >= g.B) return;
+  const int hr = (int)(id - (int64_t)b * per_seq);
+  const int h = hr / a.R, r = hr - h * a.R;
+  const SeqTokens t = seq_tokens(g, b);
+  if (t.bad && threadIdx.x == 0 && hr == 0) raise_flag(g.status, b);
+  const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+  char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head) * 2;
+  float* lse = a.lse ? a.lse + ((int64_t)b * a.heads + hq) * g.C + c : nullptr;
+  const int u = units_of(t);
+  if (u == 0) {
+    if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
+    if (lse && threadIdx.x == 0) *lse = kNegInf;
+    return;
+  }
+  const int per = units_per_team(total_units(g, lane), p.n_teams);
+  int before = 0;
+  for (int i = lane; i < b; i += 64) before += units_of(seq_tokens(g, i));
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m);
+  const int first = before / per, n = (before + u - 1) / per - first + 1;
+  if (n == 1) return;  // written whole
+  if (r >= t.nn * a.G) {
+    if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
+    if (lse && threadIdx.x == 0) *lse = kNegInf;
+    return;
+  }
+  const int64_t at = ((int64_t)(first + b) * g.H + h) * a.R + r;  // + share * H * R
+  const int64_t step = (int64_t)g.H * a.R;
+  float top = kNegInf;
+  for (int i = lane; i < n; i += 64) top = fmaxf(top, p.part_ml[at + i * step].x);
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
+  const float base2 = top == kNegInf ? 0.f : top;
+  float sum = 0.f;
+  for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    const float2 ml = p.part_ml[at + i * step];
+    const float w = exp2_fast(ml.x - base2);
+    s_w[i] = w;
+    sum += w * ml.y;
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) s_sum[wave] = sum;
+  __syncthreads();
+  float o[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = 0.f;
+  const float* po = p.part_o + at * D + lane * E;
+#pragma unroll 8
+  for (int i = wave; i < n; i += waves) {
+    const float w = s_w[i];
+    const float* x = po + i * step * D;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] += w * x[e];
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+  __syncthreads();
+  sum = 0.f;
+  for (int w = 0; w < waves; ++w) sum += s_sum[w];
+  const bool some = sum != 0.f;
+  if (threadIdx.x < D / 2) {
+    float x = 0.f, y = 0.f;
+    for (int w = 0; w < waves; ++w) {
+      x += s_o[w][2 * threadIdx.x];
+      y += s_o[w][2 * threadIdx.x + 1];
+    }
+    const float inv = 1.f / sum;
+    reinterpret_cast<uint32_t*>(op)[threadIdx.x] = some ? pack_bf16(x * inv, y * inv) : 0u;
+  }
+  if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+}
+
+// Wavefronts resident per SIMD that the shares are counted for.
+constexpr int kWavesPerSimd = 2;
+
+WavePlan wave_plan(int B, int H, int d) {
+  WavePlan p;
+  const int most = d == 256 ? 4 : 8;  // wavefronts of a workgroup (rows of 256 take 512 registers)
+  const int groups = (H + most - 1) / most;
+  p.hw = (H + groups - 1) / groups;
+  p.tpw = std::max(1, most / p.hw);
+  p.split = B <= kSplitBatch;
+  p.n_teams = B;
+  if (p.split) {
+    const int waves = std::max(1, device_cus()) * 4 * (d == 256 ? 1 : kWavesPerSimd);
+    p.n_teams = std::min(kJoinShares, (waves + p.hw * groups - 1) / (p.hw * groups));
+  }
+  p.part_o = nullptr;
+  p.part_ml = nullptr;
+  return p;
+}
+
+template <int D, int NT>
+hipError_t launch_wave(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
+  const dim3 grid = linear_grid((p.n_teams + p.tpw - 1) / p.tpw, 512, (a.pg.H + p.hw - 1) / p.hw);
+  const dim3 block(p.hw * p.tpw * 64);
+  if (q4)
+    hipLaunchKernelGGL((k_attend_wave<D, NT, true>), grid, block, 0, s, a, p);
+  else
+    hipLaunchKernelGGL((k_attend_wave<D, NT, false>), grid, block, 0, s, a, p);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !p.split) return e;
+  const int shares = p.n_teams / a.pg.B;  // of a sequence, about
+  const int waves = shares >= 64 ? 16 : shares >= 16 ? 8 : 4;
+  hipLaunchKernelGGL(k_attend_join<D>, linear_grid((int64_t)a.pg.B * a.pg.H * a.R, waves * 64),
+                     dim3(waves * 64), 0, s, a, p);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_tiles(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
+  switch (attend_wave_tiles(a.R)) {
+    case 1: return launch_wave<D, 1>(a, p, q4, s);
+    default: return launch_wave<D, 2>(a, p, q4, s);
+  }
+}
+
+size_t part_ml_bytes(const WavePlan& p, int B, int H, int R) {
+  return ((size_t)(p.n_teams + B) * H * R * sizeof(float2) + 255) / 256 * 256;
+}
+
+}  // namespace
+
+int attend_wave_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 0; }
+
+size_t attend_wave_workspace(int B, int H, int R, int d) {
+  const WavePlan p = wave_plan(B, H, d);
+  if (!p.split) return 0;
+  return part_ml_bytes(p, B, H, R) + (size_t)(p.n_teams + B) * H * R * d * sizeof(float);
+}
+
+hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s) {
+  WavePlan p = wave_plan(a.pg.B, a.pg.H, a.pg.d);
+  if (p.split) {
+    p.part_ml = (float2*)ws;
+    p.part_o = (float*)((char*)ws + part_ml_bytes(p, a.pg.B, a.pg.H, a.R));
+  }
+  if (a.pg.d == 64) return launch_tiles<64>(a, p, q4, s);
+  if (a.pg.d == 128) return launch_tiles<128>(a, p, q4, s);
+  return launch_tiles<256>(a, p, q4, s);
+}
+
+}  // namespace epikv

@@ -13,6 +13,7 @@ namespace {
 
 constexpr int kMaxChunk = 1 << 24;
 constexpr int kMaxHeads = 1024;
+constexpr int kMaxTokens = 1 << 28;  // of one sequence: sums over sequences stay in 32 bits
 
 int check_rope_cfg(const epikv_rope_cfg* r) {
   if (!r) return EPIKV_EINVAL_NULL;
@@ -151,9 +152,8 @@ PagedArgs paged_args(const epikv_cfg* c, const epikv_pool* pool, int32_t layer, 
   for (int sh = 0; sh <= 10; ++sh)
     if ((1 << sh) == c->page_size) a.page_shift = sh;
   a.row_bytes = row_bytes(c);
-  // (lengths are int32; the kernels walk past the last token by less than 1024)
-  a.max_tokens = (int32_t)std::min<int64_t>(
-      std::min<int64_t>(ld_pt, INT32_MAX) * c->page_size, INT32_MAX - 1024);
+  a.max_tokens = (int32_t)std::min<int64_t>(std::min<int64_t>(ld_pt, INT32_MAX) * c->page_size,
+                                            kMaxTokens);
   return a;
 }
 
