@@ -35,7 +35,7 @@ SOURCES = ["epikv_api.hip", "score_hs.hip", "score_lagkv.hip", "zscore.hip",
            "smooth_resolve.hip", "step_prep.hip",
            "score_select.hip", "select_multi.hip", "noalloc.hip",
            "cache_api.hip", "rope.hip", "append.hip", "attend.hip",
-           "attend_wave.hip"]
+           "attend_wave.hip", "attend_tile.hip"]
 
 ARCH = "gfx950"
 CXXFLAGS = [

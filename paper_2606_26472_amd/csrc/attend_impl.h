@@ -69,6 +69,11 @@ __device__ __forceinline__ bool word_not_finite(uint32_t w) {
   return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
 }
 
+// The lowest n bits (none for n <= 0, all for n >= 32).
+__device__ __forceinline__ uint32_t below(int n) {
+  return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1u;
+}
+
 // Lower / upper halves of two words.
 __device__ __forceinline__ uint32_t halves_lo(uint32_t lo, uint32_t hi) {
   return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
@@ -82,5 +87,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 int attend_wave_tiles(int R);  // 16-row tiles of the wavefront kernel, 0: too many rows
 size_t attend_wave_workspace(int B, int H, int R, int d);
 hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
+size_t attend_tile_workspace(int B, int H, int R, int d);
+hipError_t launch_attend_tile(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 
 }  // namespace epikv

@@ -208,11 +208,10 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = s[t][e / 4][e % 4];
       if (special) {
+        asm volatile("");  // (kept a branch: the masks are not for every step)
+        const uint32_t mine = (ok & below(lim[t] - base)) >> (4 * q4);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = (e < 4 ? 0 : 12) + 4 * q4 + e;
-          x[e] = (ok >> j & 1u) && base + j < lim[t] ? x[e] : kNegInf;
-        }
+        for (int e = 0; e < 8; ++e) x[e] = mine >> ((e < 4 ? 0 : 12) + e) & 1u ? x[e] : kNegInf;
       }
       float m = x[0];
 #pragma unroll
@@ -263,12 +262,12 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
       // infinity that some rows see and others do not (0 times it is NaN)
       // needs a pass for each token c, without the values hidden from it.
       auto masks = [&](int seen) {
+        const uint32_t mine = (ok & below(seen - base)) >> (4 * q4);
         u32x4 m;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int j = (i < 2 ? 0 : 12) + 4 * q4 + 2 * i;
-          m[i] = ((ok >> j & 1u) && base + j < seen ? 0xffffu : 0u) |
-                 ((ok >> (j + 1) & 1u) && base + j + 1 < seen ? 0xffff0000u : 0u);
+          const int j = (i < 2 ? 0 : 12) + 2 * i;
+          m[i] = (mine >> j & 1u ? 0xffffu : 0u) | (mine >> (j + 1) & 1u ? 0xffff0000u : 0u);
         }
         return m;
       };

@@ -322,7 +322,7 @@ EPIKV_EXPORT size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t c
   if (check_cfg(cfg) || chunk < 1 || chunk > kMaxChunk ||
       !heads_fit(chunk, cfg->n_kv_heads, n_heads) || (int64_t)cfg->batch * chunk > INT32_MAX)
     return 0;
-  return attend_workspace(cfg->batch, chunk, cfg->n_kv_heads, n_heads, cfg->head_dim, is_q4(cfg));
+  return attend_workspace(cfg->batch, chunk, cfg->n_kv_heads, n_heads, cfg->head_dim);
 }
 
 EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
@@ -341,7 +341,7 @@ EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
   const size_t n_out = rows_span(&io->out, B, C, io->n_heads, d, 2);
   const size_t n_q = rows_span(&io->q, B, C, io->n_heads, d, 2);
   if (overlap(io->out.base, n_out, io->q.base, n_q)) return EPIKV_EALIAS;
-  const size_t need = attend_workspace(B, C, H, io->n_heads, d, is_q4(cfg));
+  const size_t need = attend_workspace(B, C, H, io->n_heads, d);
   if (need) {
     if (!io->workspace || io->workspace_bytes < need) return EPIKV_EWORKSPACE;
     if (!aligned16(io->workspace)) return EPIKV_EALIGN;

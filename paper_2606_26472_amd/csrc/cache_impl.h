@@ -46,11 +46,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// The power of two of a 4-bit block's scale byte; 255 (a block that held a
-// NaN or an infinity) gives NaN, and with it every value of the block.
-__device__ __forceinline__ float block_scale(uint32_t byte) {
-  return __uint_as_float(byte == 255u ? 0x7fc00000u : byte << 23);
-}
+// The power of two of a 4-bit block's scale byte, as the conversion takes it:
+// its exponent alone counts, and that of 255 (a block that held a NaN or an
+// infinity) makes every value of the block NaN.
+__device__ __forceinline__ float block_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // Eight codes (two to a byte, the lower first) as bf16 times the scale, two
 // to a v_cvt_scalef32_pk_bf16_fp4.

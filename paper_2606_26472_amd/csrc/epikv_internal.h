@@ -550,7 +550,7 @@ hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
 hipError_t launch_append(const AppendArgs& a, bool q4, hipStream_t s);
 hipError_t launch_read(const ReadArgs& a, bool q4, hipStream_t s);
-size_t attend_workspace(int B, int C, int H, int heads, int d, bool q4);
+size_t attend_workspace(int B, int C, int H, int heads, int d);
 hipError_t launch_attend(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 
 // Shared host checks (epikv_api.hip).
