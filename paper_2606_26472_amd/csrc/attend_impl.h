@@ -22,11 +22,11 @@ constexpr int kUnit = 32;
 // no other (team, sequence) pair of the staircase has.
 struct WavePlan {
   int32_t n_teams;  // shares (split) or sequences
-  int32_t hw;       // KV heads a team walks side by side, a wavefront each
-  int32_t tpw;      // teams per workgroup
+  int32_t hw;       // KV heads a team (a workgroup) walks side by side, a wavefront each
   int32_t split;    // sequences are cut
   float* part_o;    // [n_teams + B][H][R][d] unnormalised
   float2* part_ml;  // [n_teams + B][H][R] maximum (base 2) and sum
+  int2* shares;     // [B] a sequence's first team and how many it has
 };
 constexpr int kSplitBatch = 256;  // largest batch whose sequences are cut
 constexpr int kMinUnits = 2;
@@ -45,15 +45,7 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
   return v;
 }
 
-// Units of all sequences (at most 2^23 each, so int32 holds their sum).
-__device__ __forceinline__ int total_units(const PagedArgs& g, int lane) {
-  int sum = 0;
-  for (int b = lane; b < g.B; b += 64) sum += units_of(seq_tokens(g, b));
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
-  return sum;
-}
-
+// (at most 2^23 units a sequence and 256 sequences: sums fit 32 bits)
 __device__ __forceinline__ int units_per_team(int total, int n_teams) {
   return max(kMinUnits, (total + n_teams - 1) / n_teams);
 }

@@ -13,95 +13,157 @@
 namespace epikv {
 namespace {
 
+// What a lane holds of 32 tokens: of each of 8 of them, VC channels.
 template <int D, bool Q4>
-struct Step {  // 32 tokens on their way from memory
-  static constexpr int KS = D / 32;   // first product: 32 channels an instruction
-  static constexpr int VC = D / 16;   // second product: channels a lane brings, instructions
-  static constexpr int KW = Q4 ? KS : KS * 4;      // words per 16-token tile
-  static constexpr int VW = Q4 ? (VC + 7) / 8 : VC / 2;  // words per token
-  uint32_t k[2][KW];
+struct Values {
+  static constexpr int VC = D / 16;  // instructions of the second product
+  static constexpr int VW = Q4 ? (VC + 7) / 8 : VC / 2;
   uint32_t v[8][VW];
-  uint32_t ks[2], vs[8];  // 4-bit rows: scale bytes
+  uint32_t scale[Q4 ? 8 : 1];
 };
 
+// 32 tokens on their way from memory.  bf16 rows come as the products take
+// them.  Of 4-bit rows a lane loads a quarter of a key and of a value of two
+// tokens, and one token's scale bytes: five loads a step, where loads as the
+// second product takes them would be 22 (with those the kernel ran at half
+// its speed); values and scales then change lanes through LDS.
 template <int D, bool Q4>
-__device__ __forceinline__ void load_k(Step<D, Q4>& st, const AttendArgs& a, const int64_t* off, int h,
-                                       int n, int g) {
-  using S = Step<D, Q4>;
+struct Step {
+  static constexpr int KS = D / 32;  // first product: 32 channels an instruction
+  uint32_t k[2][KS * 4];
+  Values<D, false> val;
+};
+template <int D>
+struct Step<D, true> {
+  static constexpr int KS = D / 32;
+  uint32_t k[2][KS], v[2][KS];
+  uint32_t sc[D == 256 ? 2 : 1];
+};
+
+// A wavefront's part of LDS.
+template <int D, bool Q4>
+struct Scratch {
+  int64_t off[kUnit];  // a step's row offsets
+};
+template <int D>
+struct Scratch<D, true> {
+  // bytes between tokens' codes: reads of 4 tokens at a time meet no bank twice
+  static constexpr int ROW = D == 64 ? 48 : D == 128 ? 80 : 160;
+  static constexpr int SB = D / 32;
+  int64_t off[kUnit];
+  __attribute__((aligned(16))) char codes[kUnit * ROW];
+  __attribute__((aligned(8))) uint8_t scales[2 * kUnit * SB];  // keys', then values'
+};
+
+// W words; ONCE marks them as not to be kept in the caches.
+template <int W, bool ONCE = false>
+__device__ __forceinline__ void load_words(uint32_t* to, const char* p) {
+  if constexpr (W == 2) {
+    const u32x2* q = reinterpret_cast<const u32x2*>(p);
+    const u32x2 w = ONCE ? __builtin_nontemporal_load(q) : *q;
+    to[0] = w[0];
+    to[1] = w[1];
+  } else {
 #pragma unroll
-  for (int t = 0; t < 2; ++t) {
-    const char* row = a.pg.plane[0] + off[16 * t + n];
-    if constexpr (Q4) {
-      const char* p = row + h * (D / 2) + g * (D / 8);
-      if constexpr (D == 64) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-        st.k[t][0] = w[0];
-        st.k[t][1] = w[1];
-      } else {
+    for (int i = 0; i < W / 4; ++i) {
+      const u32x4* q = reinterpret_cast<const u32x4*>(p + 16 * i);
+      const u32x4 w = ONCE ? __builtin_nontemporal_load(q) : *q;
 #pragma unroll
-        for (int i = 0; i < S::KW / 4; ++i) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(p + 16 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) st.k[t][4 * i + j] = w[j];
-        }
-      }
-      const uint8_t* sc = reinterpret_cast<const uint8_t*>(row) + a.pg.H * (D / 2) + h * (D / 32);
-      if constexpr (D == 64) st.ks[t] = sc[g / 2];
-      if constexpr (D == 128) st.ks[t] = sc[g];
-      if constexpr (D == 256) st.ks[t] = *reinterpret_cast<const uint16_t*>(sc + 2 * g);
-    } else {
-      const char* p = row + h * (D * 2) + g * 16;
-#pragma unroll
-      for (int i = 0; i < S::KS; ++i) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(p + 64 * i);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) st.k[t][4 * i + j] = w[j];
-      }
+      for (int j = 0; j < 4; ++j) to[4 * i + j] = w[j];
     }
   }
 }
 
-template <int D, bool Q4>
-__device__ __forceinline__ void load_v(Step<D, Q4>& st, const AttendArgs& a, const int64_t* off, int h,
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_k(Step<D, false>& st, const AttendArgs& a, const int64_t* off, int h,
                                        int n, int g) {
-  using S = Step<D, Q4>;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const char* p = a.pg.plane[0] + off[16 * t + n] + h * (D * 2) + g * 16;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) load_words<4, ONCE>(&st.k[t][4 * i], p + 64 * i);
+  }
+}
+
+template <int D, bool ONCE>
+__device__ __forceinline__ void load_v(Step<D, false>& st, const AttendArgs& a, const int64_t* off, int h,
+                                       int n, int g) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    load_words<D / 32, ONCE>(st.val.v[e], a.pg.plane[1] + off[(e < 4 ? 0 : 12) + 4 * g + e] + h * (D * 2) + n * (D / 8));
+}
+
+template <int D, bool>
+__device__ __forceinline__ void load_k(Step<D, true>& st, const AttendArgs& a, const int64_t* off, int h,
+                                       int n, int g) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    load_words<D / 32>(st.k[t], a.pg.plane[0] + off[16 * t + n] + h * (D / 2) + g * (D / 8));
+}
+
+// Values, and the scale bytes of the token whose row is at `own`: lanes below
+// 32 take its key's, the others its value's.
+template <int D, bool>
+__device__ __forceinline__ void load_v(Step<D, true>& st, const AttendArgs& a, const int64_t* off,
+                                       int64_t own, int h, int n, int g) {
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+    load_words<D / 32>(st.v[t], a.pg.plane[1] + off[16 * t + n] + h * (D / 2) + g * (D / 8));
+  const char* p = (g < 2 ? a.pg.plane[0] : a.pg.plane[1]) + own + a.pg.H * (D / 2) + h * (D / 32);
+  if constexpr (D == 64) st.sc[0] = *reinterpret_cast<const uint16_t*>(p);
+  if constexpr (D == 128) st.sc[0] = *reinterpret_cast<const uint32_t*>(p);
+  if constexpr (D == 256) load_words<2>(st.sc, p);
+}
+
+template <int D>
+__device__ __forceinline__ void stash(const Step<D, true>& st, Scratch<D, true>& lds, int lane) {
+  using L = Scratch<D, true>;
+  const int n = lane & 15, g = lane >> 4;
+  wave_sync();
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    char* p = lds.codes + (16 * t + n) * L::ROW + g * (D / 8);
+    if constexpr (D == 64) {
+      *reinterpret_cast<u32x2*>(p) = u32x2{st.v[t][0], st.v[t][1]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < D / 128; ++i)
+        *reinterpret_cast<u32x4*>(p + 16 * i) =
+            u32x4{st.v[t][4 * i], st.v[t][4 * i + 1], st.v[t][4 * i + 2], st.v[t][4 * i + 3]};
+    }
+  }
+  uint8_t* s = lds.scales + lane * L::SB;
+  if constexpr (D == 64) *reinterpret_cast<uint16_t*>(s) = (uint16_t)st.sc[0];
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(s) = st.sc[0];
+  if constexpr (D == 256) *reinterpret_cast<u32x2*>(s) = u32x2{st.sc[0], st.sc[1]};
+  wave_sync();
+}
+
+template <int D>
+__device__ __forceinline__ void fetch(Values<D, true>& x, const Scratch<D, true>& lds, int lane) {
+  using L = Scratch<D, true>;
+  const int n = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const char* row = a.pg.plane[1] + off[(e < 4 ? 0 : 12) + 4 * g + e];
-    if constexpr (Q4) {
-      const char* p = row + h * (D / 2) + n * (S::VC / 2);
-      if constexpr (D == 64) st.v[e][0] = *reinterpret_cast<const uint16_t*>(p);
-      if constexpr (D == 128) st.v[e][0] = *reinterpret_cast<const uint32_t*>(p);
-      if constexpr (D == 256) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-        st.v[e][0] = w[0];
-        st.v[e][1] = w[1];
-      }
-      st.vs[e] = reinterpret_cast<const uint8_t*>(row)[a.pg.H * (D / 2) + h * (D / 32) + n * S::VC / 32];
-    } else {
-      const char* p = row + h * (D * 2) + n * (S::VC * 2);
-      if constexpr (D == 64) {
-        const u32x2 w = *reinterpret_cast<const u32x2*>(p);
-        st.v[e][0] = w[0];
-        st.v[e][1] = w[1];
-      } else {
-#pragma unroll
-        for (int i = 0; i < S::VW / 4; ++i) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(p + 16 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) st.v[e][4 * i + j] = w[j];
-        }
-      }
+    const int tok = (e < 4 ? 0 : 12) + 4 * g + e;
+    const char* p = lds.codes + tok * L::ROW + n * (D / 32);
+    if constexpr (D == 64) x.v[e][0] = *reinterpret_cast<const uint16_t*>(p);
+    if constexpr (D == 128) x.v[e][0] = *reinterpret_cast<const uint32_t*>(p);
+    if constexpr (D == 256) {
+      const u32x2 w = *reinterpret_cast<const u32x2*>(p);
+      x.v[e][0] = w[0];
+      x.v[e][1] = w[1];
     }
+    x.scale[e] = lds.scales[(kUnit + tok) * L::SB + n * (D / 16) / 32];
   }
 }
 
 // Word w (two channels) of the values that a lane holds of token e.
 template <int D, bool Q4>
-__device__ __forceinline__ uint32_t v_word(const Step<D, Q4>& st, int e, int w) {
-  if constexpr (!Q4) return st.v[e][w];
-  const uint32_t codes = st.v[e][w / 4];
-  const float s = block_scale(st.vs[e]);
+__device__ __forceinline__ uint32_t v_word(const Values<D, Q4>& x, int e, int w) {
+  if constexpr (!Q4) return x.v[e][w];
+  const uint32_t codes = x.v[e][w / 4];
+  const float s = block_scale(x.scale[Q4 ? e : 0]);
   switch (w % 4) {
     case 0: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0));
     case 1: return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1));
@@ -110,14 +172,22 @@ __device__ __forceinline__ uint32_t v_word(const Step<D, Q4>& st, int e, int w) 
   }
 }
 
-// Units [u0, u1) of sequence b for KV head h.  `off`: this wavefront's two
-// tables of row offsets.  whole: the units are all of the sequence's, the
-// result is final; else it goes to partial slot `slot`.
+// Steps on their way at a time: what the registers hold beside the query and
+// the outputs, and enough bytes in flight for memory's latency.
 template <int D, int NT, bool Q4>
+constexpr int steps_ahead() {
+  if (Q4) return D == 64 && NT == 1 ? 3 : 2;
+  return D == 64 ? 2 : 1;
+}
+
+// Units [u0, u1) of sequence b for KV head h.  `lds`: this wavefront's
+// scratch.  whole: the units are all of the sequence's, the
+// result is final; else it goes to partial slot `slot`.
+template <int D, int NT, bool Q4, bool ONCE>
 __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
-                             int u0, int u1, bool whole, int slot, int64_t (*off)[kUnit], int lane) {
+                             int u0, int u1, bool whole, int slot, Scratch<D, Q4>& lds, int lane) {
   using S = Step<D, Q4>;
-  constexpr int KS = S::KS, VC = S::VC;
+  constexpr int KS = S::KS, VC = D / 16;
   const PagedArgs& g = a.pg;
   const int n = lane & 15, q4 = lane >> 4;
   const int rows = tk.nn * a.G;  // rows of real tokens
@@ -147,41 +217,76 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
 
   const int begin = u0 * kUnit, end = min(tk.n, u1 * kUnit);  // this share's slots (end > begin)
   const int seen_by_all = tk.n - tk.nn + 1;
+  // The page table 64 entries at a time, the next 64 on their way; tokens past
+  // the share's end stand for the last one, whose row costs no more traffic.
   const int32_t* pt = g.pt + (int64_t)b * g.ld_pt;
-  // The page entry of the token this lane stands for in a step (past the
-  // share's end: the last one's, whose row costs no more memory traffic).
   auto page_index = [&](int tok) {
     return g.page_shift >= 0 ? tok >> g.page_shift : (int)((uint32_t)tok / (uint32_t)g.page_size);
   };
+  const int last_page = page_index(end - 1);
+  auto load_pages = [&](int first) { return pt[min(first + lane, last_page)]; };
+  int page0 = page_index(begin);
+  int pages = load_pages(page0), pages_next = load_pages(page0 + 64);
   const int at32 = lane & (kUnit - 1);
-  auto load_entry = [&](int base) { return pt[page_index(min(base + at32, end - 1))]; };
   bool any_bad = false;
-  // The step's row offsets to LDS; returns which of its tokens exist.
-  auto put_offsets = [&](int base, int pg, int64_t* table) -> uint32_t {
+  int64_t own = 0;  // the row of this lane's token
+  // A step's row offsets to LDS; returns which of its tokens exist.
+  auto put_offsets = [&](int base) -> uint32_t {
+    if (page_index(min(base, end - 1)) - page0 >= 64) {
+      page0 += 64;
+      pages = pages_next;
+      pages_next = load_pages(page0 + 64);
+    }
     const int tok = min(base + at32, end - 1);
+    const int pi = page_index(tok), rel = pi - page0;
+    int pg = __shfl(pages, rel & 63);
+    if (__any(rel >= 64)) {  // (a branch, not to wait for the next entries before they are due)
+      const int beyond = __shfl(pages_next, rel & 63);
+      pg = rel < 64 ? pg : beyond;
+    }
     const bool good = pg >= 0 && pg < g.n_pages;
-    const int64_t at = (int64_t)pg * g.s_page + (int64_t)(tok - page_index(tok) * g.page_size) * g.row_bytes;
+    const int64_t at = (int64_t)pg * g.s_page + (int64_t)(tok - pi * g.page_size) * g.row_bytes;
+    own = good ? at : 0;
     wave_sync();
-    table[at32] = good ? at : 0;
+    lds.off[at32] = own;
     wave_sync();
     any_bad |= !good;
     return (uint32_t)__ballot(good && base + at32 < end);
   };
 
-  Step<D, Q4> st;
-  int entry = load_entry(begin);
-  uint32_t ok = put_offsets(begin, entry, off[0]);
-  entry = load_entry(begin + kUnit);
-  load_k<D, Q4>(st, a, off[0], h, n, q4);
-  load_v<D, Q4>(st, a, off[0], h, n, q4);
-  int buf = 0;
-  // A step takes 32 tokens; the next one's keys are on their way once this
-  // one's are used up, and so its values.
-#pragma clang loop unroll(disable)
-  for (int base = begin; base < end; base += kUnit) {
-    buf ^= 1;
-    const uint32_t ok_next = put_offsets(base + kUnit, entry, off[buf]);
-    entry = load_entry(base + 2 * kUnit);
+  constexpr int P = steps_ahead<D, NT, Q4>();
+  Step<D, Q4> steps[P];
+  uint32_t exist[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    exist[i] = put_offsets(begin + i * kUnit);
+    load_k<D, ONCE>(steps[i], a, lds.off, h, n, q4);
+    if constexpr (Q4)
+      load_v<D, ONCE>(steps[i], a, lds.off, own, h, n, q4);
+    else
+      load_v<D, ONCE>(steps[i], a, lds.off, h, n, q4);
+  }
+  // One step of 32 tokens; the keys of the one P steps on are on their way
+  // once this one's are used up, and so its values.
+  auto step = [&](Step<D, Q4>& st, uint32_t& exists, int base) {
+    const uint32_t ok = exists;
+    // 4-bit rows of two heads and more share lines: the heads' wavefronts keep
+    // together (they walk the same share, and so come here equally often), or
+    // lines leave the cache before the last of them has read its part.
+    if constexpr (Q4) __builtin_amdgcn_s_barrier();
+    uint32_t key_scale[2] = {0, 0};
+    if constexpr (Q4) stash<D>(st, lds, lane);
+    exists = put_offsets(base + P * kUnit);
+    if constexpr (Q4) {
+      load_v<D, ONCE>(st, a, lds.off, own, h, n, q4);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint8_t* x = lds.scales + (16 * i + n) * Scratch<D, true>::SB;
+        if constexpr (D == 64) key_scale[i] = x[q4 / 2];
+        if constexpr (D == 128) key_scale[i] = x[q4];
+        if constexpr (D == 256) key_scale[i] = *reinterpret_cast<const uint16_t*>(x + 2 * q4);
+      }
+    }
     f32x4 s[NT][2];
 #pragma unroll
     for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -191,7 +296,8 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
       for (int k = 0; k < KS; ++k) {
         u32x4 w;
         if constexpr (Q4) {
-          const uint32_t byte = D == 256 ? (k < KS / 2 ? st.ks[i] & 255u : st.ks[i] >> 8) : st.ks[i];
+          const uint32_t byte =
+              D == 256 ? (k < KS / 2 ? key_scale[i] & 255u : key_scale[i] >> 8) : key_scale[i];
           w = decode8(st.k[i][k], block_scale(byte));
         } else {
           w = u32x4{st.k[i][4 * k], st.k[i][4 * k + 1], st.k[i][4 * k + 2], st.k[i][4 * k + 3]};
@@ -199,7 +305,7 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
 #pragma unroll
         for (int t = 0; t < NT; ++t) s[t][i] = mfma16(as_bf16x8(w), qf[t][k], s[t][i]);
       }
-    load_k<D, Q4>(st, a, off[buf], h, n, q4);
+    load_k<D, ONCE>(st, a, lds.off, h, n, q4);
     const bool special = ok != 0xffffffffu || base + 32 > seen_by_all;
     bf16x8 pf[NT];
 #pragma unroll
@@ -239,15 +345,23 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
       pf[t] = as_bf16x8(u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]),
                               pack_bf16(w[6], w[7])});
     }
-    // V: a lane holds 8 tokens of VC channels; an instruction takes one
-    // channel's 8 tokens, two channels come of 8 words.
+    Values<D, Q4> fetched;
+    if constexpr (Q4) fetch<D>(fetched, lds, lane);
+    Values<D, Q4>& val = [&]() -> Values<D, Q4>& {
+      if constexpr (Q4)
+        return fetched;
+      else
+        return st.val;
+    }();
+    // V: an instruction takes one channel's 8 tokens, two channels come of 8
+    // words.
     if (!special) {
 #pragma unroll
       for (int w = 0; w < VC / 2; ++w) {
         u32x4 c0, c1;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+          const uint32_t x = v_word(val, 2 * i, w), y = v_word(val, 2 * i + 1, w);
           c0[i] = halves_lo(x, y);
           c1[i] = halves_hi(x, y);
         }
@@ -278,7 +392,7 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         for (int w = 0; w < VC / 2; ++w)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+            const uint32_t x = v_word(val, 2 * i, w), y = v_word(val, 2 * i + 1, w);
             odd |= word_not_finite(halves_lo(x, y) & there[i]) | word_not_finite(halves_hi(x, y) & there[i]);
           }
       }
@@ -291,13 +405,13 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int w = 0; w < S::VW; ++w) asm volatile("" : "+v"(st.v[e][w]));
+          for (int w = 0; w < Values<D, Q4>::VW; ++w) asm volatile("" : "+v"(val.v[e][w]));
 #pragma unroll
         for (int w = 0; w < VC / 2; ++w) {
           u32x4 c0, c1;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t x = v_word(st, 2 * i, w), y = v_word(st, 2 * i + 1, w);
+            const uint32_t x = v_word(val, 2 * i, w), y = v_word(val, 2 * i + 1, w);
             c0[i] = halves_lo(x, y) & m[i];
             c1[i] = halves_hi(x, y) & m[i];
           }
@@ -313,8 +427,13 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         }
       }
     }
-    load_v<D, Q4>(st, a, off[buf], h, n, q4);
-    ok = ok_next;
+    if constexpr (!Q4) load_v<D, ONCE>(st, a, lds.off, h, n, q4);
+  };
+#pragma clang loop unroll(disable)
+  for (int base = begin; base < end; base += P * kUnit) {
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (base + i * kUnit < end) step(steps[i], exist[i], base + i * kUnit);
   }
   if (__any(any_bad) && lane == 0) raise_flag(g.status, b);
 
@@ -371,15 +490,15 @@ __device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
   }
 }
 
-template <int D, int NT, bool Q4>
+template <int D, int NT, bool Q4, bool ONCE>
 __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
-  __shared__ __align__(16) int64_t s_off[8][2][kUnit];
+  __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const PagedArgs& g = a.pg;
-  const int h = blockIdx.y * p.hw + wave % p.hw;
-  const int64_t team = linear_block() * p.tpw + wave / p.hw;
-  if (h >= g.H || team >= p.n_teams) return;  // (no workgroup barrier below)
+  const int h = blockIdx.y * p.hw + wave;
+  const int64_t team = linear_block();
+  if (h >= g.H || team >= p.n_teams) return;
   if (!p.split) {
     const int b = (int)team;
     const SeqTokens t = seq_tokens(g, b);
@@ -388,37 +507,60 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
     if (u == 0)
       attend_nothing<D>(a, b, h, lane);
     else
-      attend_share<D, NT, Q4>(a, p, b, h, t, 0, u, true, 0, s_off[wave], lane);
+      attend_share<D, NT, Q4, ONCE>(a, p, b, h, t, 0, u, true, 0, s_lds[wave], lane);
     return;
   }
-  const int total = total_units(g, lane);
+  // All sequences' units, a lane each (their loads at once), and where this
+  // team's share begins among them.
+  constexpr int SETS = kSplitBatch / 64;
+  int n[SETS], nn[SETS], upto[SETS], total = 0;
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    const int b = 64 * i + lane;
+    n[i] = nn[i] = 0;
+    if (b < g.B) {
+      const SeqTokens t = seq_tokens(g, b);
+      n[i] = t.n;
+      nn[i] = t.nn;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    if (64 * i >= g.B) break;
+    upto[i] = total + wave_scan(units_of(SeqTokens{n[i], nn[i], false}), lane);
+    total = __builtin_amdgcn_readlane(upto[i], 63);
+  }
   const int per = units_per_team(total, p.n_teams);
   int lo = (int)team * per;
   const int hi = min(total, lo + per);
   if (lo >= hi) return;
-  // the sequence that holds unit lo, and the units before it
-  int b0 = 0, before = 0;
-  for (;; b0 += 64) {
-    const int b = b0 + lane;
-    const int u = b < g.B ? units_of(seq_tokens(g, b)) : 0;
-    const int upto = before + wave_scan(u, lane);
-    const uint64_t past = __ballot(upto > lo);
+  int b = 0, before = 0;
+  SeqTokens t = {0, 0, false};
+#pragma unroll
+  for (int i = 0; i < SETS; ++i) {
+    if (64 * i >= g.B || t.nn > 0) break;
+    const uint64_t past = __ballot(upto[i] > lo);
     if (past) {
       const int k = __ffsll((unsigned long long)past) - 1;
-      before = __builtin_amdgcn_readlane(upto - u, k);
-      b0 += k;
-      break;
+      t.n = __builtin_amdgcn_readlane(n[i], k);
+      t.nn = __builtin_amdgcn_readlane(nn[i], k);
+      before = __builtin_amdgcn_readlane(upto[i], k) - units_of(t);
+      b = 64 * i + k;
     }
-    before = __builtin_amdgcn_readlane(upto, 63);
   }
-  for (int b = __builtin_amdgcn_readfirstlane(b0); lo < hi; ++b) {
-    const SeqTokens t = seq_tokens(g, b);
+  for (;;) {
     const int u = units_of(t);
-    if (u == 0) continue;
-    const int u0 = lo - before, u1 = min(u, hi - before);
-    attend_share<D, NT, Q4>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_off[wave], lane);
-    lo = before + u1;
-    before += u;
+    if (u > 0) {
+      const int u0 = lo - before, u1 = min(u, hi - before);
+      // (who has a sequence's first unit tells the join where its shares are)
+      if (u0 == 0 && h == 0 && lane == 0)
+        p.shares[b] = make_int2((int)team, (before + u - 1) / per - (int)team + 1);
+      attend_share<D, NT, Q4, ONCE>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_lds[wave], lane);
+      lo = before + u1;
+      before += u;
+    }
+    if (lo >= hi) break;
+    t = seq_tokens(g, ++b);
   }
 }
 
@@ -440,6 +582,7 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
   if (b >= g.B) return;
   const int hr = (int)(id - (int64_t)b * per_seq);
   const int h = hr / a.R, r = hr - h * a.R;
+  const int2 at_first = p.shares[b];  // (nothing there if the sequence has no units)
   const SeqTokens t = seq_tokens(g, b);
   if (t.bad && threadIdx.x == 0 && hr == 0) raise_flag(g.status, b);
   const int c = r / a.G, hq = h * a.G + (r - c * a.G);
@@ -451,12 +594,7 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
     if (lse && threadIdx.x == 0) *lse = kNegInf;
     return;
   }
-  const int per = units_per_team(total_units(g, lane), p.n_teams);
-  int before = 0;
-  for (int i = lane; i < b; i += 64) before += units_of(seq_tokens(g, i));
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) before += __shfl_xor(before, m);
-  const int first = before / per, n = (before + u - 1) / per - first + 1;
+  const int first = at_first.x, n = at_first.y;
   if (n == 1) return;  // written whole
   if (r >= t.nn * a.G) {
     if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
@@ -509,6 +647,12 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
   if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
+// bf16 rows are not kept in the caches when the page tables cover more than the
+// last-level cache holds: 32 sequences of 8k-32k tokens 453 -> 415 us.  Fewer
+// may still be there at the next token: 4224 slots 16.7 us kept, 18.5 not.
+// (4-bit rows share lines between wavefronts and are kept: no difference.)
+constexpr int64_t kCacheBytes = 256 << 20;
+
 // Wavefronts resident per SIMD that the shares are counted for.
 constexpr int kWavesPerSimd = 2;
 
@@ -517,7 +661,6 @@ WavePlan wave_plan(int B, int H, int d) {
   const int most = d == 256 ? 4 : 8;  // wavefronts of a workgroup (rows of 256 take 512 registers)
   const int groups = (H + most - 1) / most;
   p.hw = (H + groups - 1) / groups;
-  p.tpw = std::max(1, most / p.hw);
   p.split = B <= kSplitBatch;
   p.n_teams = B;
   if (p.split) {
@@ -526,17 +669,20 @@ WavePlan wave_plan(int B, int H, int d) {
   }
   p.part_o = nullptr;
   p.part_ml = nullptr;
+  p.shares = nullptr;
   return p;
 }
 
 template <int D, int NT>
 hipError_t launch_wave(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
-  const dim3 grid = linear_grid((p.n_teams + p.tpw - 1) / p.tpw, 512, (a.pg.H + p.hw - 1) / p.hw);
-  const dim3 block(p.hw * p.tpw * 64);
+  const dim3 grid = linear_grid(p.n_teams, p.hw * 64, (a.pg.H + p.hw - 1) / p.hw);
+  const dim3 block(p.hw * 64);
   if (q4)
-    hipLaunchKernelGGL((k_attend_wave<D, NT, true>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, NT, true, false>), grid, block, 0, s, a, p);
+  else if ((int64_t)a.pg.B * a.pg.max_tokens * 2 * a.pg.row_bytes > kCacheBytes)
+    hipLaunchKernelGGL((k_attend_wave<D, NT, false, true>), grid, block, 0, s, a, p);
   else
-    hipLaunchKernelGGL((k_attend_wave<D, NT, false>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, NT, false, false>), grid, block, 0, s, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
   const int shares = p.n_teams / a.pg.B;  // of a sequence, about
@@ -558,6 +704,8 @@ size_t part_ml_bytes(const WavePlan& p, int B, int H, int R) {
   return ((size_t)(p.n_teams + B) * H * R * sizeof(float2) + 255) / 256 * 256;
 }
 
+constexpr size_t kSharesBytes = kSplitBatch * sizeof(int2);
+
 }  // namespace
 
 int attend_wave_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 0; }
@@ -565,14 +713,15 @@ int attend_wave_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 0; }
 size_t attend_wave_workspace(int B, int H, int R, int d) {
   const WavePlan p = wave_plan(B, H, d);
   if (!p.split) return 0;
-  return part_ml_bytes(p, B, H, R) + (size_t)(p.n_teams + B) * H * R * d * sizeof(float);
+  return kSharesBytes + part_ml_bytes(p, B, H, R) + (size_t)(p.n_teams + B) * H * R * d * sizeof(float);
 }
 
 hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s) {
   WavePlan p = wave_plan(a.pg.B, a.pg.H, a.pg.d);
   if (p.split) {
-    p.part_ml = (float2*)ws;
-    p.part_o = (float*)((char*)ws + part_ml_bytes(p, a.pg.B, a.pg.H, a.R));
+    p.shares = (int2*)ws;
+    p.part_ml = (float2*)((char*)ws + kSharesBytes);
+    p.part_o = (float*)((char*)p.part_ml + part_ml_bytes(p, a.pg.B, a.pg.H, a.R));
   }
   if (a.pg.d == 64) return launch_tiles<64>(a, p, q4, s);
   if (a.pg.d == 128) return launch_tiles<128>(a, p, q4, s);
