@@ -16,20 +16,31 @@ __device__ __forceinline__ uint32_t block_byte(uint32_t top_bits) {
   return (uint32_t)max(e, 1);
 }
 
-// e2m1 code of |x| in units, to nearest, ties to the even code, 7 (6.0) at
-// most: the values' midpoints.
-__device__ __forceinline__ uint32_t e2m1(float x) {
-  const float v = fabsf(x);
-  uint32_t c = (v > 0.25f) + (v >= 0.75f) + (v > 1.25f) + (v >= 1.75f) + (v > 2.5f) + (v >= 3.5f) +
-               (v > 5.0f);
-  return c | (__float_as_uint(x) >> 31 << 3);
-}
-
-// Eight channels of one head of a new token's key or value, four lanes to a
-// block of 32.
-template <bool Q4>
-__device__ __forceinline__ void append_vec(const AppendArgs& a, int b, int c, int kv, int h, int vec) {
+// Eight channels of U heads h, h + step, ... of a new token's keys or values
+// (kv), four lanes to a block of 32.  A key's partner channels are read again
+// rather than exchanged (they are in the cache), so that every layout and
+// rotary_dim is one code.
+template <bool Q4, int U>
+__device__ __forceinline__ void append_vecs(const AppendArgs& a, int b, int c, int kv, int h, int step,
+                                            int vec) {
   const PagedArgs& g = a.pg;
+  const RowsArg& in = kv ? a.v : a.k;
+  const char* x = in.base + (b * in.ld_seq + c * in.ld_tok + h * in.ld_head) * 2;
+  const int64_t next = step * in.ld_head * 2;
+  const int r = a.rope.r;
+  const bool rot = kv == 0 && a.rope.table && vec * 8 < r;
+  const bool half = rot && !a.rope.interleaved;
+  const int nv = r / 16;  // vectors per half
+  const bool upper = half && vec >= nv;
+  const int first = upper ? vec - nv : vec;
+  u32x4 own[U], partner[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) own[i] = *reinterpret_cast<const u32x4*>(x + i * next + vec * 16);
+  if (half) {
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      partner[i] = *reinterpret_cast<const u32x4*>(x + i * next + (upper ? first : vec + nv) * 16);
+  }
   const SeqTokens t = seq_tokens(g, b);
   if (c >= t.nn) {
     if (t.bad) raise_flag(g.status, b);
@@ -47,141 +58,179 @@ __device__ __forceinline__ void append_vec(const AppendArgs& a, int b, int c, in
   }
   if (kv == 0 && h == 0 && vec == 0 && a.pos && slot < a.ld_s)
     a.pos[(int64_t)b * a.ld_s + slot] = (int32_t)p;
-  const RowsArg& in = kv ? a.v : a.k;
-  const char* x = in.base + (b * in.ld_seq + c * in.ld_tok + h * in.ld_head) * 2;
-  float u[8];
-  u32x4 raw = *reinterpret_cast<const u32x4*>(x + vec * 16);
-  unpack8(raw, u);
-  const int r = a.rope.r;
-  const bool rot = kv == 0 && a.rope.table && vec * 8 < r;
+  f32x4 cs[4];
   if (rot) {
-    const float2* row = a.rope.table + p * (r / 2);
-    if (a.rope.interleaved) {
-      const f32x4* t4 = reinterpret_cast<const f32x4*>(row + vec * 4);
-      const f32x4 cs[2] = {t4[0], t4[1]};
+    const f32x4* t4 = reinterpret_cast<const f32x4*>(a.rope.table + p * (r / 2) + (half ? first * 8 : vec * 4));
+    cs[0] = t4[0];
+    cs[1] = t4[1];
+    if (half) {
+      cs[2] = t4[2];
+      cs[3] = t4[3];
+    }
+  }
+  char* row = g.plane[kv] + off;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        rotate_pair(u[2 * i], u[2 * i + 1], f32x2{cs[i / 2][2 * (i % 2)], cs[i / 2][2 * (i % 2) + 1]},
-                    false);
-    } else {
-      const int nv = r / 16;  // vectors per half
-      const bool upper = vec >= nv;
-      const int first = upper ? vec - nv : vec;
+  for (int k = 0; k < U; ++k) {
+    float u[8];
+    unpack8(own[k], u);
+    if (half) {
       float w[8];
-      unpack8(*reinterpret_cast<const u32x4*>(x + (upper ? first : vec + nv) * 16), w);
-      const f32x4* t4 = reinterpret_cast<const f32x4*>(row + first * 8);
-      const f32x4 cs[4] = {t4[0], t4[1], t4[2], t4[3]};
+      unpack8(partner[k], w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float lo = upper ? w[i] : u[i], hi = upper ? u[i] : w[i];
-        rotate_pair(lo, hi, f32x2{cs[i / 2][2 * (i % 2)], cs[i / 2][2 * (i % 2) + 1]}, false);
+        rotate_pair(lo, hi, pair_of(cs, i), false);
         u[i] = upper ? hi : lo;
       }
+    } else if (rot) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) rotate_pair(u[2 * i], u[2 * i + 1], pair_of(cs, i), false);
     }
-    raw = pack8(u);
-  }
-  char* row = g.plane[kv] + off;
-  if constexpr (!Q4) {
-    *reinterpret_cast<u32x4*>(row + (h * g.d + vec * 8) * 2) = raw;
-  } else {
-    // (integer order of magnitudes: NaN and infinity sort above all numbers)
-    uint32_t top = 0;
+    const int head = h + k * step;
+    if constexpr (!Q4) {
+      st_stream(row + (head * g.d + vec * 8) * 2, rot ? pack8(u) : own[k]);
+    } else {
+      // (integer order of magnitudes: NaN and infinity sort above all numbers)
+      uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(u[i]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const uint32_t byte = block_byte(top);
-    const float inv = __uint_as_float((254u - min(byte, 253u)) << 23);
-    uint32_t codes = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) codes |= e2m1(u[i] * inv) << (4 * i);
-    *reinterpret_cast<uint32_t*>(row + h * (g.d / 2) + vec * 4) = codes;
-    if ((vec & 3) == 0) row[g.H * (g.d / 2) + h * (g.d / 32) + vec / 4] = (char)byte;
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(u[i]) & 0x7fffffffu);
+      top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0xB1, 0xF, 0xF, false));  // lane ^ 1
+      top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, 0x4E, 0xF, 0xF, false));  // lane ^ 2
+      const uint32_t byte = block_byte(top);
+      const float s = block_scale(byte);
+      // (to nearest, ties to the even code, at most 6)
+      uint32_t codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, u[0], u[1], s, 0);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[2], u[3], s, 1);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[4], u[5], s, 2);
+      codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, u[6], u[7], s, 3);
+      *reinterpret_cast<uint32_t*>(row + head * (g.d / 2) + vec * 4) = byte == 255u ? 0u : codes;
+      if ((vec & 3) == 0) row[g.H * (g.d / 2) + head * (g.d / 32) + vec / 4] = (char)byte;
+    }
   }
 }
 
-// A thread per item: 16 channels of a query head (rope_item), or 8 of a key
-// or value head.  Block roles: the first nq_blocks rotate queries.
-template <bool Q4>
-__global__ __launch_bounds__(256) void k_append(AppendArgs a, int64_t nq_blocks) {
+// Bound by HBM (long chunks: 205 MB in 37.7 us, 5.4 TB/s) or by the launch and
+// the chain of loads to a row (single tokens: 4.5 us).
+//
+// Queries: a thread per two vectors of UQ heads (rope_items), in the first
+// nq_blocks workgroups; keys and values: a thread per 8 channels of UKV heads.
+template <bool Q4, bool WAVE, int UQ, int UKV>
+__global__ __launch_bounds__(256) void k_append(AppendArgs a, int64_t nq_blocks, int per_q, int per_kv) {
   const PagedArgs& g = a.pg;
   const int64_t block = linear_block();
+  const int64_t tokens = (int64_t)g.B * g.C;
   if (block < nq_blocks) {
-    const int64_t t = block * 256 + threadIdx.x;
-    const int iph = g.d / 16, ipt = a.heads * iph;
-    const int64_t token = t / ipt;
-    if (token >= (int64_t)g.B * g.C) return;
-    const int it = (int)(t - token * ipt);
-    const int b = (int)(token / g.C), c = (int)(token - (int64_t)b * g.C);
+    const Place at = place_of<WAVE>(block, per_q, tokens);
+    if (!at.in) return;
+    const int b = at.token / g.C, c = at.token - b * g.C;
     if (c >= seq_tokens(g, b).nn) return;
-    const int h = it / iph;
-    rope_item<false>(a.q, a.q_out, a.rope, g.status, b, c, h, it - h * iph);
+    const int iph = g.d / 16, h = at.item / iph;
+    rope_items<false, UQ>(a.q, a.q_out, a.rope, g.status, b, c, h, a.heads / UQ, at.item - h * iph, g.d);
     return;
   }
-  const int64_t t = (block - nq_blocks) * 256 + threadIdx.x;
-  const int vph = g.d / 8, vpt = 2 * g.H * vph;
-  const int64_t token = t / vpt;
-  if (token >= (int64_t)g.B * g.C) return;
-  const int it = (int)(t - token * vpt);
-  const int b = (int)(token / g.C), c = (int)(token - (int64_t)b * g.C);
-  const int kv = it / (g.H * vph);
-  const int hv = it - kv * g.H * vph;
-  append_vec<Q4>(a, b, c, kv, hv / vph, hv % vph);
+  const Place at = place_of<WAVE>(block - nq_blocks, per_kv, tokens);
+  if (!at.in) return;
+  const int b = at.token / g.C, c = at.token - b * g.C;
+  const int vph = g.d / 8, heads = g.H / UKV;
+  const int hv = at.item / vph, kv = hv / heads;
+  append_vecs<Q4, UKV>(a, b, c, kv, hv - kv * heads, heads, at.item - hv * vph);
 }
 
-// Rows back: a thread per 8 channels.
-template <bool Q4>
-__global__ __launch_bounds__(256) void k_read(ReadArgs a) {
+// Rows back: a thread per 8 channels of U heads.
+template <bool Q4, bool WAVE, int U>
+__global__ __launch_bounds__(256) void k_read(ReadArgs a, int per) {
   const PagedArgs& g = a.pg;
-  const int64_t t = linear_block() * 256 + threadIdx.x;
-  const int vph = g.d / 8, vpt = 2 * g.H * vph;
-  const int64_t token = t / vpt;
-  if (token >= (int64_t)g.B * g.C) return;
-  const int it = (int)(t - token * vpt);
-  const int b = (int)(token / g.C), c = (int)(token - (int64_t)b * g.C);
-  const int kv = it / (g.H * vph);
-  const int hv = it - kv * g.H * vph;
-  const int h = hv / vph, vec = hv % vph;
+  const Place at = place_of<WAVE>(linear_block(), per, (int64_t)g.B * g.C);
+  if (!at.in) return;
+  const int b = at.token / g.C, c = at.token - b * g.C;
+  const int vph = g.d / 8, heads = g.H / U;
+  const int hv = at.item / vph, kv = hv / heads, h = hv - kv * heads, vec = at.item - hv * vph;
   const RowsArg& out = kv ? a.v : a.k;
   if (!out.base) return;
   const int64_t slot = (int64_t)g.n_cached[b] + c;
   const int64_t off = slot >= 0 && slot < g.max_tokens ? row_offset(g, b, (int)slot) : -1;
-  u32x4 w = {0, 0, 0, 0};
-  if (off < 0) {
-    raise_flag(g.status, b);
-  } else {
-    const char* row = g.plane[kv] + off;
+  if (off < 0) raise_flag(g.status, b);
+  const char* row = g.plane[kv] + max(off, (int64_t)0);
+  u32x4 w[U];
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    const int head = h + i * heads;
     if constexpr (Q4) {
-      const uint32_t codes = *reinterpret_cast<const uint32_t*>(row + h * (g.d / 2) + vec * 4);
-      const uint8_t byte = (uint8_t)row[g.H * (g.d / 2) + h * (g.d / 32) + vec / 4];
-      w = decode8(codes, block_scale(byte));
+      const uint32_t codes = *reinterpret_cast<const uint32_t*>(row + head * (g.d / 2) + vec * 4);
+      const uint8_t byte = (uint8_t)row[g.H * (g.d / 2) + head * (g.d / 32) + vec / 4];
+      w[i] = decode8(codes, block_scale(byte));
     } else {
-      w = *reinterpret_cast<const u32x4*>(row + (h * g.d + vec * 8) * 2);
+      w[i] = *reinterpret_cast<const u32x4*>(row + (head * g.d + vec * 8) * 2);
     }
+    if (off < 0) w[i] = u32x4{0, 0, 0, 0};
   }
-  *reinterpret_cast<u32x4*>(out.base + (b * out.ld_seq + c * out.ld_tok + h * out.ld_head + vec * 8) * 2) = w;
+  char* o = out.base + (b * out.ld_seq + c * out.ld_tok + h * out.ld_head + vec * 8) * 2;
+#pragma unroll
+  for (int i = 0; i < U; ++i) st_stream(o + i * heads * out.ld_head * 2, w[i]);
+}
+
+// Heads a thread takes, of queries as of keys and values: the way to a token's
+// row (its counts, its page, its position) is as long for one as for two.  A
+// prompt of 8191 tokens (32 query heads, 8 KV heads of 128) takes 45.8 us with
+// one of each, 39.3 with two KV heads, 37.7 with two of each, 39.1 with four
+// query heads.
+int heads_at_once(int heads) { return heads % 2 == 0 ? 2 : 1; }
+
+template <bool Q4, int UQ, int UKV>
+void launch_append_heads(const AppendArgs& a, hipStream_t s) {
+  const int64_t tokens = (int64_t)a.pg.B * a.pg.C;
+  const int per_q = a.q.base ? a.heads / UQ * (a.pg.d / 16) : 64;
+  const int per_kv = 2 * (a.pg.H / UKV) * (a.pg.d / 8);
+  const int64_t nq = a.q.base ? (tokens * per_q + 255) / 256 : 0;
+  const dim3 grid = linear_grid(nq + (tokens * per_kv + 255) / 256, 256);
+  if (per_q % 64 == 0 && per_kv % 64 == 0)
+    hipLaunchKernelGGL((k_append<Q4, true, UQ, UKV>), grid, dim3(256), 0, s, a, nq, per_q, per_kv);
+  else
+    hipLaunchKernelGGL((k_append<Q4, false, UQ, UKV>), grid, dim3(256), 0, s, a, nq, per_q, per_kv);
+}
+
+template <bool Q4, int UKV>
+void launch_append_kv(const AppendArgs& a, hipStream_t s) {
+  if (a.q.base && heads_at_once(a.heads) == 2)
+    launch_append_heads<Q4, 2, UKV>(a, s);
+  else
+    launch_append_heads<Q4, 1, UKV>(a, s);
+}
+
+template <bool Q4>
+hipError_t launch_append_fmt(const AppendArgs& a, hipStream_t s) {
+  if (heads_at_once(a.pg.H) == 2)
+    launch_append_kv<Q4, 2>(a, s);
+  else
+    launch_append_kv<Q4, 1>(a, s);
+  return hipGetLastError();
+}
+
+template <bool Q4, int U>
+hipError_t launch_read_heads(const ReadArgs& a, hipStream_t s) {
+  const int per = 2 * (a.pg.H / U) * (a.pg.d / 8);
+  const dim3 grid = linear_grid(((int64_t)a.pg.B * a.pg.C * per + 255) / 256, 256);
+  if (per % 64 == 0)
+    hipLaunchKernelGGL((k_read<Q4, true, U>), grid, dim3(256), 0, s, a, per);
+  else
+    hipLaunchKernelGGL((k_read<Q4, false, U>), grid, dim3(256), 0, s, a, per);
+  return hipGetLastError();
 }
 
 }  // namespace
 
+bool append_fits(int64_t tokens, int H, int heads, int d) {
+  return threads_fit(tokens, 2 * (H / heads_at_once(H)) * (d / 8)) &&
+         (heads == 0 || threads_fit(tokens, heads / heads_at_once(heads) * (d / 16)));
+}
+
 hipError_t launch_append(const AppendArgs& a, bool q4, hipStream_t s) {
-  const int64_t tokens = (int64_t)a.pg.B * a.pg.C;
-  const int64_t nq = a.q.base ? (tokens * a.heads * (a.pg.d / 16) + 255) / 256 : 0;
-  const int64_t nkv = (tokens * 2 * a.pg.H * (a.pg.d / 8) + 255) / 256;
-  if (q4)
-    hipLaunchKernelGGL(k_append<true>, linear_grid(nq + nkv, 256), dim3(256), 0, s, a, nq);
-  else
-    hipLaunchKernelGGL(k_append<false>, linear_grid(nq + nkv, 256), dim3(256), 0, s, a, nq);
-  return hipGetLastError();
+  return q4 ? launch_append_fmt<true>(a, s) : launch_append_fmt<false>(a, s);
 }
 
 hipError_t launch_read(const ReadArgs& a, bool q4, hipStream_t s) {
-  const int64_t n = ((int64_t)a.pg.B * a.pg.C * 2 * a.pg.H * (a.pg.d / 8) + 255) / 256;
-  if (q4)
-    hipLaunchKernelGGL(k_read<true>, linear_grid(n, 256), dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(k_read<false>, linear_grid(n, 256), dim3(256), 0, s, a);
-  return hipGetLastError();
+  if (heads_at_once(a.pg.H) == 2) return q4 ? launch_read_heads<true, 2>(a, s) : launch_read_heads<false, 2>(a, s);
+  return q4 ? launch_read_heads<true, 1>(a, s) : launch_read_heads<false, 1>(a, s);
 }
 
 }  // namespace epikv

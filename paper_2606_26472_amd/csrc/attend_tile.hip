@@ -11,6 +11,8 @@
 //
 // Bound by the matrix cores and the softmax's arithmetic together (32 scores
 // a lane and tile: 32 exponentials beside 32 matrix instructions).
+#include <type_traits>
+
 #include "attend_impl.h"
 
 namespace epikv {
@@ -36,14 +38,15 @@ struct Tile {
   static constexpr int BYTES = KT * D * 2;
   // Chunks change places within a row so that the lanes that read together
   // hit different banks: keys are read at one chunk of 16 rows, values at
-  // four chunks (a 64-byte run) of 4 rows.  The change is an exclusive or of
+  // four chunks (a 64-byte run) of 4 rows (and the change within a run keeps
+  // the writes of decoded rows apart).  The change is an exclusive or of
   // the chunk's number, so a fragment's address is a lane's base address,
   // exclusive or the fragment's offset in the row, plus its rows' offset.
   __device__ static int key_chunk(int row, int c) {
     return c ^ (D == 64 ? (row >> 1) & 7 : row & 15);
   }
   __device__ static int value_chunk(int row, int c) {
-    return c ^ (D == 64 ? ((row >> 1) & 1) << 2 : (row & 3) << 2);
+    return c ^ (D == 64 ? (row >> 1) & 1 : row & 3) * 5;
   }
 };
 
@@ -86,10 +89,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
   const bool real = r < rows;
   const int old = tk.n - tk.nn;  // slots before the new tokens
   const int lim = real ? old + c + 1 : 0;
-  // slots seen by any row of the workgroup and of the wavefront, by all of the latter
+  // slots seen by any row of the workgroup and of the wavefront, by all of the former
   const int end_wg = r0 < rows ? old + (min(r0 + kRows, rows) - 1) / a.G + 1 : 0;
   const int end_w = w0 < rows ? old + (min(w0 + 32, rows) - 1) / a.G + 1 : 0;
-  const int all_w = old + w0 / a.G + 1;
+  const int all_wg = old + r0 / a.G + 1;
   const int tiles = (end_wg + KT - 1) / KT;
   const int t0 = (int)((int64_t)tiles * piece / p.splits);
   const int t1 = (int)((int64_t)tiles * (piece + 1) / p.splits);
@@ -217,23 +220,23 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
     return w;
   };
 
-  auto work = [&](int t, int buf, uint64_t ok) {
+  // A tile; MASKED: some of its tokens are hidden from some rows or do not exist.
+  auto work = [&](auto masked, int t, int buf, uint64_t ok) {
+    constexpr bool MASKED = decltype(masked)::value;
     const uint32_t kt = k_base + buf * 2 * T::BYTES;
     const uint32_t vt = v_base + buf * 2 * T::BYTES;
     const int base = t * KT;
     f32x16 s[TB];
 #pragma unroll
-    for (int i = 0; i < TB; ++i) {
+    for (int i = 0; i < TB; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+    // (in an order in which neighbours do not add to the same result)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s[i] = mfma32(key_frag(kt, i, k), qf[k], s[i]);
-    }
-    constexpr uint64_t FULL = KT == 64 ? ~0ull : 0xffffffffull;
-    ok &= FULL;
-    const bool special = ok != FULL || base + KT > all_w;
-    if (special) {
-      asm volatile("");  // (kept a branch: the masks are not for every tile)
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < TB; ++i) s[i] = mfma32(key_frag(kt, i, k), qf[k], s[i]);
+    if constexpr (MASKED) {
 #pragma unroll
       for (int i = 0; i < TB; ++i) {
         const uint32_t seen = (uint32_t)(ok >> (32 * i)) & below(lim - base - 32 * i);
@@ -273,11 +276,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
         pf[2 * i + u] = as_bf16x8(u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]),
                                         pack_bf16(w[4], w[5]), pack_bf16(w[6], w[7])});
       }
-    if (!special) {
+    if constexpr (!MASKED) {
 #pragma unroll
-      for (int j = 0; j < CT; ++j)
+      for (int k = 0; k < PS; ++k)
 #pragma unroll
-        for (int k = 0; k < PS; ++k) o[j] = mfma32(as_bf16x8(value_frag(vt, j, k)), pf[k], o[j]);
+        for (int j = 0; j < CT; ++j) o[j] = mfma32(as_bf16x8(value_frag(vt, j, k)), pf[k], o[j]);
       return;
     }
     // What does not exist counts as 0, whatever its bytes are.  A NaN or an
@@ -331,8 +334,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
     }
     int entry = load_entry(t0 + 1);
     arrived();
-    for (int t = t0; t < t1; ++t) {
-      const int buf = (t - t0) & 1;
+    int t = t0, buf = 0;
+    auto turn = [&](auto masked) {
       uint64_t ok_next = 0;
       if (t + 1 < t1) {
         ok_next = offsets(t + 1, entry);
@@ -342,13 +345,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
         else
           stage(buf ^ 1);
       }
-      if (t * KT < end_w) work(t, buf, ok);
+      if (t * KT < end_w) work(masked, t, buf, ok);
       if constexpr (Q4) {
         if (t + 1 < t1) decode(buf ^ 1);
       }
       ok = ok_next;
+      ++t;
+      buf ^= 1;
       arrived();
-    }
+    };
+    // The tiles that every row sees whole, then (from the first that is not
+    // so) the others: both conditions are the workgroup's.
+    constexpr uint64_t FULL = KT == 64 ? ~0ull : 0xffffffffull;
+    while (t < t1 && (t + 1) * KT <= all_wg && (ok & FULL) == FULL) turn(std::false_type{});
+    while (t < t1) turn(std::true_type{});
     if (__any(any_bad) && threadIdx.x == 0) raise_flag(g.status, b);
   }
 

@@ -218,6 +218,7 @@ EPIKV_EXPORT int epikv_rope(const epikv_rope_cfg* rope, const float* table, int3
   if (n_heads < 1 || n_heads > kMaxHeads) return EPIKV_EINVAL_SHAPE;
   if (head_dim < 16 || head_dim > 1024 || head_dim % 16 || rope->rotary_dim > head_dim)
     return EPIKV_EINVAL_SHAPE;
+  if (!rope_fits((int64_t)batch * chunk, n_heads, head_dim)) return EPIKV_EINVAL_SHAPE;
   if (!aligned16(table)) return EPIKV_EALIGN;
   st = check_rows(x);
   if (st) return st;
@@ -278,6 +279,7 @@ EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
          overlap(io->q_out.base, nq, io->v.base, rows_span(&io->v, B, C, H, d, 2))))
       return EPIKV_EALIAS;
   }
+  if (!append_fits((int64_t)B * C, H, io->q.base ? io->n_heads : 0, d)) return EPIKV_EINVAL_SHAPE;
   AppendArgs a;
   memset(&a, 0, sizeof(a));
   a.pg = paged_args(cfg, &io->pool, io->layer, C, io->page_table, io->ld_pt, io->n_cached,
@@ -309,6 +311,7 @@ EPIKV_EXPORT int epikv_read(const epikv_cfg* cfg, const epikv_read_io* io, hipSt
       overlap(io->k.base, rows_span(&io->k, B, C, H, d, 2), io->v.base,
               rows_span(&io->v, B, C, H, d, 2)))
     return EPIKV_EALIAS;
+  if (!append_fits((int64_t)B * C, H, 0, d)) return EPIKV_EINVAL_SHAPE;
   ReadArgs a;
   a.pg = paged_args(cfg, &io->pool, io->layer, C, io->page_table, io->ld_pt, io->first, nullptr,
                     io->seq_status);

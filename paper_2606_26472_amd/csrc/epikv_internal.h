@@ -548,6 +548,8 @@ struct AttendArgs {
 
 hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
+bool rope_fits(int64_t tokens, int heads, int d);  // one launch reaches it all
+bool append_fits(int64_t tokens, int H, int heads, int d);
 hipError_t launch_append(const AppendArgs& a, bool q4, hipStream_t s);
 hipError_t launch_read(const ReadArgs& a, bool q4, hipStream_t s);
 size_t attend_workspace(int B, int C, int H, int heads, int d);

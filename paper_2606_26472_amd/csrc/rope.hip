@@ -37,19 +37,32 @@ __global__ __launch_bounds__(256) void k_rope_table(RopeTableArgs a) {
   a.table[2 * t + 1] = (float)(a.amplitude * s);
 }
 
-// A thread per item: 16 channels of one head, the two 8-vectors whose pairs
-// belong together (or two plain ones past rotary_dim), so a rotation in place
-// reads all that it overwrites.
+// A thread per two 16-byte vectors of a head (rope_items): what a rotation in
+// place overwrites it has read.  (Two or four heads a thread share a read of
+// the table, which the cache serves as well: 45.0 and 46.3 against 45.3 us for
+// 16384 tokens of 32 heads of 128, 44.6 and 45.7 against 43.5 in float32.)
+//
+// Bound by HBM: every byte of x once and of y once, past the caches; 6.1 TB/s
+// there.
+template <bool FP32, bool WAVE>
+__global__ __launch_bounds__(256) void k_rope(RopeArgs a, int per) {
+  const Place at = place_of<WAVE>(linear_block(), per, (int64_t)a.B * a.C);
+  if (!at.in) return;
+  const int b = at.token / a.C, c = at.token - b * a.C;
+  const int iph = a.d / (FP32 ? 8 : 16);
+  const int h = at.item / iph;
+  rope_items<FP32, 1>(a.x, a.y, a.rope, a.status, b, c, h, 0, at.item - h * iph, a.d);
+}
+
 template <bool FP32>
-__global__ __launch_bounds__(256) void k_rope(RopeArgs a, int ipt, int tpb) {
-  const int tk = ipt <= 256 ? threadIdx.x / ipt : 0;
-  const int it = ipt <= 256 ? threadIdx.x - tk * ipt : (int)(blockIdx.y * 256 + threadIdx.x);
-  const int64_t token = linear_block() * tpb + tk;
-  if (tk >= tpb || it >= ipt || token >= (int64_t)a.B * a.C) return;
-  const int b = (int)(token / a.C), c = (int)(token - (int64_t)b * a.C);
-  const int iph = a.d / 16;
-  const int h = it / iph;
-  rope_item<FP32>(a.x, a.y, a.rope, a.status, b, c, h, it - h * iph);
+hipError_t launch_rope_type(const RopeArgs& a, hipStream_t s) {
+  const int per = a.heads * (a.d / (FP32 ? 8 : 16));
+  const dim3 grid = linear_grid(((int64_t)a.B * a.C * per + 255) / 256, 256);
+  if (per % 64 == 0)
+    hipLaunchKernelGGL((k_rope<FP32, true>), grid, dim3(256), 0, s, a, per);
+  else
+    hipLaunchKernelGGL((k_rope<FP32, false>), grid, dim3(256), 0, s, a, per);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -60,16 +73,12 @@ hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+bool rope_fits(int64_t tokens, int heads, int d) {
+  return threads_fit(tokens, heads * (d / 8));
+}
+
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
-  const int ipt = a.heads * (a.d / 16);
-  const int tpb = ipt <= 256 ? 256 / ipt : 1;
-  const int64_t tokens = (int64_t)a.B * a.C;
-  const dim3 grid = linear_grid((tokens + tpb - 1) / tpb, 256, ipt <= 256 ? 1 : (ipt + 255) / 256);
-  if (a.fp32)
-    hipLaunchKernelGGL(k_rope<true>, grid, dim3(256), 0, s, a, ipt, tpb);
-  else
-    hipLaunchKernelGGL(k_rope<false>, grid, dim3(256), 0, s, a, ipt, tpb);
-  return hipGetLastError();
+  return a.fp32 ? launch_rope_type<true>(a, s) : launch_rope_type<false>(a, s);
 }
 
 }  // namespace epikv

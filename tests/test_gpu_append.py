@@ -133,7 +133,7 @@ def test_append(E, shape, il, fmt):
                 assert np.array_equal(f64(back[kv][b]), held, equal_nan=True)
 
 
-@pytest.mark.parametrize("scale", [2.0 ** -100, 1e-30, 1e-3, 1.0, 1e4, 1e30, 3e38])
+@pytest.mark.parametrize("scale", [2.0 ** -127, 2.0 ** -100, 1e-30, 1e-3, 1.0, 1e4, 1e30, 3e38])
 def test_quantising_every_magnitude(E, scale):
     """Values, not rotated, over the whole range of bf16, with ties and zeros."""
     g = torch.Generator().manual_seed(11)
