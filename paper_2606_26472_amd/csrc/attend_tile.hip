@@ -1,7 +1,8 @@
 // Attention for many query rows per KV head (prefill, long chunks): a
-// workgroup takes 128 rows of one KV head, 32 to a wavefront, and walks the
-// slots in tiles of 64 whose key and value rows pass through LDS as bf16, the
-// next tile on its way while one is worked on.
+// workgroup takes 256 rows of one KV head (128 when there are no more, or rows
+// of 256 channels), 32 to a wavefront, and walks the slots in tiles of 64 whose
+// key and value rows pass through LDS as bf16, the next tile on its way while
+// one is worked on.
 //
 // As with few rows, S^T = K Q^T and O^T = V^T P^T, here with v_mfma 32x32x16:
 // lane (n, g) = (lane % 32, lane / 32) holds query row n, and of each 16
@@ -23,9 +24,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-constexpr int kRows = 128;     // query rows of a workgroup
-constexpr int kTileWaves = 4;
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -58,9 +56,10 @@ struct TilePlan {
   float2* part_ml;  // [splits][B][H][R]
 };
 
-template <int D, bool Q4>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArgs a, TilePlan p) {
+template <int D, bool Q4, int W>
+__global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_attend_tile(AttendArgs a, TilePlan p) {
   using T = Tile<D>;
+  constexpr int kRows = 32 * W;
   constexpr int KT = T::KT, KS = D / 16, CT = D / 32, TB = KT / 32, PS = KT / 16;
   __shared__ __align__(1024) char s_kv[2][2][T::BYTES];  // [buffer][K, V]
   const PagedArgs& g = a.pg;
@@ -114,19 +113,33 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
     for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
   float top = kNegInf, sum = 0.f;
 
-  // Page entries: this lane's token of a tile (past the end: the last one).
+  // The page table 64 entries at a time, the next 64 on their way; tokens past
+  // the end stand for the last one.
   const int32_t* pt = g.pt + (int64_t)b * g.ld_pt;
   auto page_index = [&](int tok) {
     return g.page_shift >= 0 ? tok >> g.page_shift : (int)((uint32_t)tok / (uint32_t)g.page_size);
   };
-  auto load_entry = [&](int t) { return pt[page_index(min(t * KT + (lane & (KT - 1)), end_wg - 1))]; };
+  const int last_page = page_index(max(end_wg - 1, 0));
+  auto load_pages = [&](int first) { return pt[min(first + lane, last_page)]; };
+  int page0 = page_index(t0 * KT), pages = 0, pages_next = 0;
   bool any_bad = false;
-  int64_t my_off = 0;
-  auto offsets = [&](int t, int pg) -> uint64_t {
+  int64_t my_off = 0;  // the row of this lane's token of the tile to be loaded
+  auto offsets = [&](int t) -> uint64_t {
     const int tok = t * KT + (lane & (KT - 1));
-    const int at = min(tok, end_wg - 1);
+    const int at = min(tok, end_wg - 1), pi = page_index(at);
+    if (page_index(min(t * KT, end_wg - 1)) - page0 >= 64) {
+      page0 += 64;
+      pages = pages_next;
+      pages_next = load_pages(page0 + 64);
+    }
+    const int rel = pi - page0;
+    int pg = __shfl(pages, rel & 63);
+    if (__any(rel >= 64)) {
+      const int beyond = __shfl(pages_next, rel & 63);
+      pg = rel < 64 ? pg : beyond;
+    }
     const bool good = pg >= 0 && pg < g.n_pages;
-    my_off = good ? (int64_t)pg * g.s_page + (int64_t)(at - page_index(at) * g.page_size) * g.row_bytes : 0;
+    my_off = good ? (int64_t)pg * g.s_page + (int64_t)(at - pi * g.page_size) * g.row_bytes : 0;
     any_bad |= !good;
     return __ballot(good && tok < end_wg);
   };
@@ -139,10 +152,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
   // bf16 rows go to LDS directly, 1 KiB an instruction.
   auto stage = [&](int buf) {
     constexpr int RPI = 1024 / (D * 2);           // rows an instruction
-    constexpr int NI = KT / kTileWaves / RPI;
+    constexpr int NI = KT / W / RPI;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const int first = wave * (KT / kTileWaves) + i * RPI;
+      const int first = wave * (KT / W) + i * RPI;
       const int row = first + lane / T::RC, cpos = lane % T::RC;
       const int64_t off = offset_of(row) + h * (D * 2);
       __builtin_amdgcn_global_load_lds(
@@ -154,7 +167,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
     }
   };
   // 4-bit rows pass through registers: a thread decodes CH channels of one token.
-  constexpr int TPT = 256 / KT, CH = D / TPT;
+  constexpr int TPT = 64 * W / KT, CH = D / TPT;
   const int q_row = threadIdx.x / TPT, q_part = threadIdx.x % TPT;
   uint32_t raw[2][CH / 8];
   uint32_t raw_s[2] = {0, 0};
@@ -164,7 +177,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
     for (int kv = 0; kv < 2; ++kv) {
       const char* row = g.plane[kv] + off;
       const char* x = row + h * (D / 2) + q_part * (CH / 2);
-      if constexpr (CH == 16) {
+      if constexpr (CH == 8) {
+        raw[kv][0] = *reinterpret_cast<const uint32_t*>(x);
+      } else if constexpr (CH == 16) {
         const u32x2 w = *reinterpret_cast<const u32x2*>(x);
         raw[kv][0] = w[0];
         raw[kv][1] = w[1];
@@ -325,21 +340,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_tile(AttendArg
   };
 
   if (t0 < t1) {
-    uint64_t ok = offsets(t0, load_entry(t0));
+    pages = load_pages(page0);
+    pages_next = load_pages(page0 + 64);
+    uint64_t ok = offsets(t0);
     if constexpr (Q4) {
       fetch();
       decode(0);
     } else {
       stage(0);
     }
-    int entry = load_entry(t0 + 1);
     arrived();
     int t = t0, buf = 0;
     auto turn = [&](auto masked) {
       uint64_t ok_next = 0;
       if (t + 1 < t1) {
-        ok_next = offsets(t + 1, entry);
-        entry = load_entry(t + 2);
+        ok_next = offsets(t + 1);
         if constexpr (Q4)
           fetch();
         else
@@ -441,12 +456,17 @@ __global__ __launch_bounds__(256) void k_attend_tile_join(AttendArgs a, TilePlan
 
 constexpr int kMaxSplits = 16;
 
-// Pieces: as many as give every compute unit two workgroups.
-TilePlan tile_plan(int B, int H, int R) {
+// Wavefronts of a workgroup: eight halve what each of them does to bring a tile
+// to LDS (a 4096-token chunk over 16k slots 1008 us with four, 914 with eight).
+int tile_waves(int R, int d) { return d <= 128 && R > 128 ? 8 : 4; }
+
+// Pieces: as many as give every compute unit eight wavefronts.
+TilePlan tile_plan(int B, int H, int R, int d) {
   TilePlan p;
-  p.row_tiles = (R + kRows - 1) / kRows;
+  const int waves = tile_waves(R, d);
+  p.row_tiles = (R + 32 * waves - 1) / (32 * waves);
   const int64_t blocks = (int64_t)B * H * p.row_tiles;
-  const int64_t want = 2 * (int64_t)std::max(1, device_cus());
+  const int64_t want = (int64_t)std::max(1, device_cus()) * 8 / waves;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, want / blocks));
   p.part_o = nullptr;
   p.part_ml = nullptr;
@@ -459,13 +479,25 @@ size_t part_ml_bytes(const TilePlan& p, int B, int H, int R) {
   return (part_rows(p, B, H, R) * sizeof(float2) + 255) / 256 * 256;
 }
 
+template <int D, int W>
+void launch_tile_waves(const AttendArgs& a, const TilePlan& p, bool q4, hipStream_t s) {
+  const dim3 grid = linear_grid((int64_t)a.pg.B * a.pg.H * p.row_tiles * p.splits, 64 * W);
+  if (q4)
+    hipLaunchKernelGGL((k_attend_tile<D, true, W>), grid, dim3(64 * W), 0, s, a, p);
+  else
+    hipLaunchKernelGGL((k_attend_tile<D, false, W>), grid, dim3(64 * W), 0, s, a, p);
+}
+
 template <int D>
 hipError_t launch_tile(const AttendArgs& a, const TilePlan& p, bool q4, hipStream_t s) {
-  const dim3 grid = linear_grid((int64_t)a.pg.B * a.pg.H * p.row_tiles * p.splits, 256);
-  if (q4)
-    hipLaunchKernelGGL((k_attend_tile<D, true>), grid, dim3(256), 0, s, a, p);
-  else
-    hipLaunchKernelGGL((k_attend_tile<D, false>), grid, dim3(256), 0, s, a, p);
+  if constexpr (D <= 128) {
+    if (tile_waves(a.R, D) == 8)
+      launch_tile_waves<D, 8>(a, p, q4, s);
+    else
+      launch_tile_waves<D, 4>(a, p, q4, s);
+  } else {
+    launch_tile_waves<D, 4>(a, p, q4, s);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(k_attend_tile_join<D>,
@@ -476,13 +508,13 @@ hipError_t launch_tile(const AttendArgs& a, const TilePlan& p, bool q4, hipStrea
 }  // namespace
 
 size_t attend_tile_workspace(int B, int H, int R, int d) {
-  const TilePlan p = tile_plan(B, H, R);
+  const TilePlan p = tile_plan(B, H, R, d);
   if (p.splits == 1) return 0;
   return part_ml_bytes(p, B, H, R) + part_rows(p, B, H, R) * d * sizeof(float);
 }
 
 hipError_t launch_attend_tile(const AttendArgs& a, bool q4, void* ws, hipStream_t s) {
-  TilePlan p = tile_plan(a.pg.B, a.pg.H, a.R);
+  TilePlan p = tile_plan(a.pg.B, a.pg.H, a.R, a.pg.d);
   if (p.splits > 1) {
     p.part_ml = (float2*)ws;
     p.part_o = (float*)((char*)ws + part_ml_bytes(p, a.pg.B, a.pg.H, a.R));
