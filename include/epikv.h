@@ -566,7 +566,7 @@ int epikv_evict_step_noalloc(const epikv_cfg* cfg, const epikv_step_io* io,
  * seq_status (int32 [B], optional) is only raised here: a sequence with
  * something out of range gets EPIKV_SEQ_RANGE, no call lowers a flag.
  * Out of range are: n_new[b] outside [0, chunk], n_cached[b] outside
- * [n_new[b], min(ld_pt*page_size, 2^28)] (the sequence counts as having no
+ * [n_new[b], min(ld_pt*page_size, 2^25)] (the sequence counts as having no
  * tokens), a
  * page id outside [0, n_pages) (its tokens are neither written nor read, and
  * attention leaves them out) and a position outside [0, n_pos) (the token is

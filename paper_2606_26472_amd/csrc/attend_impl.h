@@ -16,8 +16,9 @@ constexpr float kNegInf = -__builtin_inff();
 constexpr int kUnit = 32;
 
 // One sequence's units are cut over several teams of wavefronts when the
-// batch is small: all sequences' units in a row, cut into even shares of at
-// least kMinUnits, so that ragged lengths cost no balance.  A team's share may
+// batch is small: all sequences' units in a row, cut into even shares (of one
+// unit at least: 4224 slots 16.5 us in shares of two, 15.3 of one), so that
+// ragged lengths cost no balance.  A team's share may
 // span sequences; its part of sequence b goes to partial slot team + b, which
 // no other (team, sequence) pair of the staircase has.
 struct WavePlan {
@@ -28,8 +29,7 @@ struct WavePlan {
   float2* part_ml;  // [n_teams + B][H][R] maximum (base 2) and sum
   int2* shares;     // [B] a sequence's first team and how many it has
 };
-constexpr int kSplitBatch = 256;  // largest batch whose sequences are cut
-constexpr int kMinUnits = 2;
+constexpr int kSplitBatch = 1024;  // largest batch whose sequences are cut
 
 __device__ __forceinline__ int units_of(const SeqTokens& t) {
   return t.nn > 0 ? (t.n + kUnit - 1) / kUnit : 0;
@@ -45,9 +45,8 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
   return v;
 }
 
-// (at most 2^23 units a sequence and 256 sequences: sums fit 32 bits)
 __device__ __forceinline__ int units_per_team(int total, int n_teams) {
-  return max(kMinUnits, (total + n_teams - 1) / n_teams);
+  return max(1, (total + n_teams - 1) / n_teams);
 }
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
@@ -76,7 +75,10 @@ __device__ __forceinline__ uint32_t halves_hi(uint32_t lo, uint32_t hi) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-int attend_wave_tiles(int R);  // 16-row tiles of the wavefront kernel, 0: too many rows
+// Query rows per KV head up to which the wavefront kernel is taken: the columns
+// of one of its instructions.  (At 32 rows of 128 channels over 8 x 8192 slots
+// it takes 103 us with two sets of them, the tile kernel 71; at 16 rows 67.)
+constexpr int kWaveRows = 16;
 size_t attend_wave_workspace(int B, int H, int R, int d);
 hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 size_t attend_tile_workspace(int B, int H, int R, int d);

@@ -51,7 +51,7 @@ struct Tile {
 // How the rows are dealt out: row tiles of every (sequence, KV head), each
 // walked whole or in `splits` even pieces (partial slots [splits][B]).
 struct TilePlan {
-  int32_t row_tiles, splits;
+  int32_t row_tiles, splits, waves, paired;
   float* part_o;    // [splits][B][H][R][d]
   float2* part_ml;  // [splits][B][H][R]
 };
@@ -67,13 +67,16 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_attend_tile(Attend
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int n = lane & 31, gh = lane >> 5;
 
-  // (heads first: workgroups side by side in the launch go to different XCDs,
-  // so that those of one head share an XCD's cache; the last, longest rows of
-  // a chunk start first)
+  // Heads first: workgroups side by side in the launch go to different XCDs,
+  // so that those of one head share an XCD's cache.  The last, longest rows of
+  // a chunk start first; when all rows are under way at once (`paired`), the
+  // second half comes shortest first, so that a compute unit's two workgroups
+  // have as much to do as any other's.
   int64_t id = linear_block();
   const int h = (int)(id % g.H);
   id /= g.H;
-  const int rt = p.row_tiles - 1 - (int)(id % p.row_tiles);
+  const int k = (int)(id % p.row_tiles);
+  const int rt = p.paired && 2 * k >= p.row_tiles ? k - (p.row_tiles + 1) / 2 : p.row_tiles - 1 - k;
   id /= p.row_tiles;
   const int piece = (int)(id % p.splits);
   const int64_t bb = id / p.splits;
@@ -435,7 +438,7 @@ __global__ __launch_bounds__(256) void k_attend_tile_join(AttendArgs a, TilePlan
     for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[at + s * step].x);
     for (int s = 0; s < p.splits; ++s) {
       const float2 ml = p.part_ml[at + s * step];
-      if (ml.x == kNegInf) continue;
+      if (ml.x == kNegInf && ml.y == 0.f) continue;  // (nothing seen; a NaN sum stays)
       const float w = exp2_fast(ml.x - top);
       sum += w * ml.y;
       const float* x = p.part_o + (at + s * step) * D + lane * E;
@@ -458,16 +461,24 @@ constexpr int kMaxSplits = 16;
 
 // Wavefronts of a workgroup: eight halve what each of them does to bring a tile
 // to LDS (a 4096-token chunk over 16k slots 1008 us with four, 914 with eight).
-int tile_waves(int R, int d) { return d <= 128 && R > 128 ? 8 : 4; }
-
+// Four where eight would leave one workgroup of uneven rows to each compute
+// unit, in chunks of many row tiles (a prompt of 2048 tokens, 32 tiles, whose
+// first rows see little and whose last see all: 76.7 us with eight, 71.9 with
+// four, 67.5 with those in pairs; 1500 tokens after 1500, 24 tiles: 107.5,
+// 103.6, 102.6; but 1000 alone, 16 tiles: 44.5, 49.4, 49.0, and 512 after 7680,
+// 8 tiles: 98, 107, 110).
 // Pieces: as many as give every compute unit eight wavefronts.
 TilePlan tile_plan(int B, int H, int R, int d) {
   TilePlan p;
-  const int waves = tile_waves(R, d);
-  p.row_tiles = (R + 32 * waves - 1) / (32 * waves);
+  const int64_t cus = std::max(1, device_cus());
+  auto tiles = [&](int waves) { return (R + 32 * waves - 1) / (32 * waves); };
+  p.waves = d <= 128 && R > 128 ? 8 : 4;
+  if (p.waves == 8 && tiles(8) >= 24 && (int64_t)B * H * tiles(8) < 2 * cus) p.waves = 4;
+  p.row_tiles = tiles(p.waves);
   const int64_t blocks = (int64_t)B * H * p.row_tiles;
-  const int64_t want = (int64_t)std::max(1, device_cus()) * 8 / waves;
+  const int64_t want = cus * 8 / p.waves;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, want / blocks));
+  p.paired = p.waves == 4 && p.splits == 1 && B == 1 && blocks <= want;
   p.part_o = nullptr;
   p.part_ml = nullptr;
   return p;
@@ -491,7 +502,7 @@ void launch_tile_waves(const AttendArgs& a, const TilePlan& p, bool q4, hipStrea
 template <int D>
 hipError_t launch_tile(const AttendArgs& a, const TilePlan& p, bool q4, hipStream_t s) {
   if constexpr (D <= 128) {
-    if (tile_waves(a.R, D) == 8)
+    if (p.waves == 8)
       launch_tile_waves<D, 8>(a, p, q4, s);
     else
       launch_tile_waves<D, 4>(a, p, q4, s);

@@ -174,16 +174,15 @@ __device__ __forceinline__ uint32_t v_word(const Values<D, Q4>& x, int e, int w)
 
 // Steps on their way at a time: what the registers hold beside the query and
 // the outputs, and enough bytes in flight for memory's latency.
-template <int D, int NT, bool Q4>
+template <int D, bool Q4>
 constexpr int steps_ahead() {
-  if (Q4) return D == 64 && NT == 1 ? 3 : 2;
+  if (Q4) return D == 64 ? 3 : 2;
   return D == 64 ? 2 : 1;
 }
 
-// Units [u0, u1) of sequence b for KV head h.  `lds`: this wavefront's
-// scratch.  whole: the units are all of the sequence's, the
-// result is final; else it goes to partial slot `slot`.
-template <int D, int NT, bool Q4, bool ONCE>
+// Units [u0, u1) of sequence b for KV head h.  whole: the units are all of the
+// sequence's, the result is final; else it goes to partial slot `slot`.
+template <int D, bool Q4, bool ONCE>
 __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
                              int u0, int u1, bool whole, int slot, Scratch<D, Q4>& lds, int lane) {
   using S = Step<D, Q4>;
@@ -191,30 +190,6 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
   const PagedArgs& g = a.pg;
   const int n = lane & 15, q4 = lane >> 4;
   const int rows = tk.nn * a.G;  // rows of real tokens
-  bf16x8 qf[NT][KS];
-  f32x4 o[NT][VC];
-  float top[NT], sum[NT];
-  int lim[NT];  // slots this lane's row sees
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const int r = t * 16 + n;
-    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
-    const bool real = r < rows;
-    const char* qp = a.q.base + (b * a.q.ld_seq + c * a.q.ld_tok + hq * a.q.ld_head) * 2;
-    lim[t] = real ? tk.n - tk.nn + c + 1 : 0;
-    top[t] = kNegInf;
-    sum[t] = 0.f;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int ch = Q4 ? (D / 4) * q4 + 8 * s : 32 * s + 8 * q4;
-      u32x4 w = {0, 0, 0, 0};
-      if (real) w = *reinterpret_cast<const u32x4*>(qp + ch * 2);
-      qf[t][s] = as_bf16x8(w);
-    }
-#pragma unroll
-    for (int j = 0; j < VC; ++j) o[t][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
   const int begin = u0 * kUnit, end = min(tk.n, u1 * kUnit);  // this share's slots (end > begin)
   const int seen_by_all = tk.n - tk.nn + 1;
   // The page table 64 entries at a time, the next 64 on their way; tokens past
@@ -227,6 +202,25 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
   auto load_pages = [&](int first) { return pt[min(first + lane, last_page)]; };
   int page0 = page_index(begin);
   int pages = load_pages(page0), pages_next = load_pages(page0 + 64);
+
+  bf16x8 qf[KS];
+  f32x4 o[VC];
+  float top = kNegInf, sum = 0.f;
+  const int r = n;  // this lane's row
+  const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+  const bool real = r < rows;
+  const char* qp = a.q.base + (b * a.q.ld_seq + c * a.q.ld_tok + hq * a.q.ld_head) * 2;
+  const int lim = real ? tk.n - tk.nn + c + 1 : 0;  // slots it sees
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    const int ch = Q4 ? (D / 4) * q4 + 8 * s : 32 * s + 8 * q4;
+    u32x4 w = {0, 0, 0, 0};
+    if (real) w = *reinterpret_cast<const u32x4*>(qp + ch * 2);
+    qf[s] = as_bf16x8(w);
+  }
+#pragma unroll
+  for (int j = 0; j < VC; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
   const int at32 = lane & (kUnit - 1);
   bool any_bad = false;
   int64_t own = 0;  // the row of this lane's token
@@ -254,7 +248,7 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
     return (uint32_t)__ballot(good && base + at32 < end);
   };
 
-  constexpr int P = steps_ahead<D, NT, Q4>();
+  constexpr int P = steps_ahead<D, Q4>();
   Step<D, Q4> steps[P];
   uint32_t exist[P];
 #pragma unroll
@@ -287,9 +281,7 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         if constexpr (D == 256) key_scale[i] = *reinterpret_cast<const uint16_t*>(x + 2 * q4);
       }
     }
-    f32x4 s[NT][2];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -302,49 +294,45 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         } else {
           w = u32x4{st.k[i][4 * k], st.k[i][4 * k + 1], st.k[i][4 * k + 2], st.k[i][4 * k + 3]};
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) s[t][i] = mfma16(as_bf16x8(w), qf[t][k], s[t][i]);
+        s[i] = mfma16(as_bf16x8(w), qf[k], s[i]);
       }
     load_k<D, ONCE>(st, a, lds.off, h, n, q4);
     const bool special = ok != 0xffffffffu || base + 32 > seen_by_all;
-    bf16x8 pf[NT];
+    bf16x8 pf;
+    float x[8];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float x[8];
+    for (int e = 0; e < 8; ++e) x[e] = s[e / 4][e % 4];
+    if (special) {
+      asm volatile("");  // (kept a branch: the masks are not for every step)
+      const uint32_t mine = (ok & below(lim - base)) >> (4 * q4);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = s[t][e / 4][e % 4];
-      if (special) {
-        asm volatile("");  // (kept a branch: the masks are not for every step)
-        const uint32_t mine = (ok & below(lim[t] - base)) >> (4 * q4);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = mine >> ((e < 4 ? 0 : 12) + e) & 1u ? x[e] : kNegInf;
-      }
-      float m = x[0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
-      m *= a.scale2;
-      // The maximum may lag by 2^8: weights up to 256 lose nothing, and most
-      // steps then exchange and rescale nothing.
-      if (__any(m > top[t] + 8.f)) {
-        m = fmaxf(m, __shfl_xor(m, 16));
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float grown = fmaxf(top[t], m);
-        const float f = grown == top[t] ? 1.f : exp2_fast(top[t] - grown);
-        top[t] = grown;
-        sum[t] *= f;
-#pragma unroll
-        for (int j = 0; j < VC; ++j) o[t][j] *= f;
-      }
-      const float base2 = top[t] == kNegInf ? 0.f : top[t];
-      float w[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        w[e] = exp2_fast(fmaf(x[e], a.scale2, -base2));
-        sum[t] += w[e];
-      }
-      pf[t] = as_bf16x8(u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]),
-                              pack_bf16(w[6], w[7])});
+      for (int e = 0; e < 8; ++e) x[e] = mine >> ((e < 4 ? 0 : 12) + e) & 1u ? x[e] : kNegInf;
     }
+    float m = x[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) m = fmaxf(m, x[e]);
+    m *= a.scale2;
+    // The maximum may lag by 2^8: weights up to 256 lose nothing, and most
+    // steps then exchange and rescale nothing.
+    if (__any(m > top + 8.f)) {
+      m = fmaxf(m, __shfl_xor(m, 16));
+      m = fmaxf(m, __shfl_xor(m, 32));
+      const float grown = fmaxf(top, m);
+      const float f = grown == top ? 1.f : exp2_fast(top - grown);
+      top = grown;
+      sum *= f;
+#pragma unroll
+      for (int j = 0; j < VC; ++j) o[j] *= f;
+    }
+    const float base2 = top == kNegInf ? 0.f : top;
+    float w[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      w[e] = exp2_fast(fmaf(x[e], a.scale2, -base2));
+      sum += w[e];
+    }
+    pf = as_bf16x8(u32x4{pack_bf16(w[0], w[1]), pack_bf16(w[2], w[3]), pack_bf16(w[4], w[5]),
+                            pack_bf16(w[6], w[7])});
     Values<D, Q4> fetched;
     if constexpr (Q4) fetch<D>(fetched, lds, lane);
     Values<D, Q4>& val = [&]() -> Values<D, Q4>& {
@@ -365,11 +353,8 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
           c0[i] = halves_lo(x, y);
           c1[i] = halves_hi(x, y);
         }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          o[t][2 * w] = mfma16(as_bf16x8(c0), pf[t], o[t][2 * w]);
-          o[t][2 * w + 1] = mfma16(as_bf16x8(c1), pf[t], o[t][2 * w + 1]);
-        }
+        o[2 * w] = mfma16(as_bf16x8(c0), pf, o[2 * w]);
+        o[2 * w + 1] = mfma16(as_bf16x8(c1), pf, o[2 * w + 1]);
       }
     } else {
       // What does not exist counts as 0, whatever its bytes are.  A NaN or an
@@ -415,14 +400,11 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
             c0[i] = halves_lo(x, y) & m[i];
             c1[i] = halves_hi(x, y) & m[i];
           }
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const f32x4 y0 = mfma16(as_bf16x8(c0), pf[t], o[t][2 * w]);
-            const f32x4 y1 = mfma16(as_bf16x8(c1), pf[t], o[t][2 * w + 1]);
-            if (!by_token || lim[t] == seen) {
-              o[t][2 * w] = y0;
-              o[t][2 * w + 1] = y1;
-            }
+          const f32x4 y0 = mfma16(as_bf16x8(c0), pf, o[2 * w]);
+          const f32x4 y1 = mfma16(as_bf16x8(c1), pf, o[2 * w + 1]);
+          if (!by_token || lim == seen) {
+            o[2 * w] = y0;
+            o[2 * w + 1] = y1;
           }
         }
       }
@@ -437,44 +419,38 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
   }
   if (__any(any_bad) && lane == 0) raise_flag(g.status, b);
 
+  sum += __shfl_xor(sum, 16);
+  sum += __shfl_xor(sum, 32);
+  if (r >= a.R) return;
+  // (lane (n, q4) holds channels D/4*q4 + VC*i + j of row r)
+  if (whole) {
+    const bool some = real && sum != 0.f;
+    const float inv = 1.f / sum;
+    char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head + (D / 4) * q4) * 2;
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    sum[t] += __shfl_xor(sum[t], 16);
-    sum[t] += __shfl_xor(sum[t], 32);
-    const int r = t * 16 + n;
-    if (r >= a.R) continue;
-    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
-    const bool real = r < rows;
-    // (lane (n, q4) holds channels D/4*q4 + VC*i + j of row r)
-    if (whole) {
-      const bool some = real && sum[t] != 0.f;
-      const float inv = 1.f / sum[t];
-      char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head + (D / 4) * q4) * 2;
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < VC; j += 4) {
-          u32x2 w = {0u, 0u};
-          if (some) {
-            w[0] = pack_bf16(o[t][j][i] * inv, o[t][j + 1][i] * inv);
-            w[1] = pack_bf16(o[t][j + 2][i] * inv, o[t][j + 3][i] * inv);
-          }
-          *reinterpret_cast<u32x2*>(op + (VC * i + j) * 2) = w;
+      for (int j = 0; j < VC; j += 4) {
+        u32x2 w = {0u, 0u};
+        if (some) {
+          w[0] = pack_bf16(o[j][i] * inv, o[j + 1][i] * inv);
+          w[1] = pack_bf16(o[j + 2][i] * inv, o[j + 3][i] * inv);
         }
-      if (a.lse && q4 == 0)
-        a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
-            some ? (top[t] + __builtin_amdgcn_logf(sum[t])) * kLn2 : kNegInf;
-    } else if (real) {
-      const int64_t at = ((int64_t)slot * g.H + h) * a.R + r;
-      float* po = p.part_o + at * D + (D / 4) * q4;
+        *reinterpret_cast<u32x2*>(op + (VC * i + j) * 2) = w;
+      }
+    if (a.lse && q4 == 0)
+      a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
+          some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+  } else if (real) {
+    const int64_t at = ((int64_t)slot * g.H + h) * a.R + r;
+    float* po = p.part_o + at * D + (D / 4) * q4;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < VC; j += 4)
-          *reinterpret_cast<f32x4*>(po + VC * i + j) =
-              f32x4{o[t][j][i], o[t][j + 1][i], o[t][j + 2][i], o[t][j + 3][i]};
-      if (q4 == 0) p.part_ml[at] = make_float2(top[t], sum[t]);
-    }
+      for (int j = 0; j < VC; j += 4)
+        *reinterpret_cast<f32x4*>(po + VC * i + j) =
+            f32x4{o[j][i], o[j + 1][i], o[j + 2][i], o[j + 3][i]};
+    if (q4 == 0) p.part_ml[at] = make_float2(top, sum);
   }
 }
 
@@ -490,7 +466,7 @@ __device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
   }
 }
 
-template <int D, int NT, bool Q4, bool ONCE>
+template <int D, bool Q4, bool ONCE>
 __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
   __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -507,7 +483,7 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
     if (u == 0)
       attend_nothing<D>(a, b, h, lane);
     else
-      attend_share<D, NT, Q4, ONCE>(a, p, b, h, t, 0, u, true, 0, s_lds[wave], lane);
+      attend_share<D, Q4, ONCE>(a, p, b, h, t, 0, u, true, 0, s_lds[wave], lane);
     return;
   }
   // All sequences' units, a lane each (their loads at once), and where this
@@ -526,9 +502,11 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
   }
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
-    if (64 * i >= g.B) break;
-    upto[i] = total + wave_scan(units_of(SeqTokens{n[i], nn[i], false}), lane);
-    total = __builtin_amdgcn_readlane(upto[i], 63);
+    upto[i] = total;
+    if (64 * i < g.B) {
+      upto[i] += wave_scan(units_of(SeqTokens{n[i], nn[i], false}), lane);
+      total = __builtin_amdgcn_readlane(upto[i], 63);
+    }
   }
   const int per = units_per_team(total, p.n_teams);
   int lo = (int)team * per;
@@ -538,9 +516,8 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
   SeqTokens t = {0, 0, false};
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
-    if (64 * i >= g.B || t.nn > 0) break;
     const uint64_t past = __ballot(upto[i] > lo);
-    if (past) {
+    if (past && t.nn == 0) {
       const int k = __ffsll((unsigned long long)past) - 1;
       t.n = __builtin_amdgcn_readlane(n[i], k);
       t.nn = __builtin_amdgcn_readlane(nn[i], k);
@@ -555,7 +532,7 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
       // (who has a sequence's first unit tells the join where its shares are)
       if (u0 == 0 && h == 0 && lane == 0)
         p.shares[b] = make_int2((int)team, (before + u - 1) / per - (int)team + 1);
-      attend_share<D, NT, Q4, ONCE>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_lds[wave], lane);
+      attend_share<D, Q4, ONCE>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_lds[wave], lane);
       lo = before + u1;
       before += u;
     }
@@ -565,85 +542,95 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
 }
 
 // Joins the shares of one row: a workgroup per (sequence, query row), its
-// wavefronts taking turns over the shares, in a fixed order.
-constexpr int kJoinShares = 2048;  // (teams are fewer)
+// wavefronts taking turns over the shares, eight at a time, in a fixed order,
+// and then their results.  Bound by latency: after the shares' place two round
+// trips (a pass for the maximum and one for the sums took a third).
+constexpr int kMaxTeams = 2048;
 
 template <int D>
 __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) {
-  constexpr int E = D / 64;
-  __shared__ float s_w[kJoinShares];
+  constexpr int E = D / 64, AHEAD = 8;
   __shared__ float s_o[16][D];
-  __shared__ float s_sum[16];
+  __shared__ float s_top[16], s_sum[16];
   const PagedArgs& g = a.pg;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int64_t id = linear_block();
-  const int per_seq = a.R * g.H;
+  const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const uint32_t id = (uint32_t)linear_block(), per_seq = (uint32_t)(a.R * g.H);
   const int b = (int)(id / per_seq);
   if (b >= g.B) return;
-  const int hr = (int)(id - (int64_t)b * per_seq);
+  const int hr = (int)(id - (uint32_t)b * per_seq);
   const int h = hr / a.R, r = hr - h * a.R;
-  const int2 at_first = p.shares[b];  // (nothing there if the sequence has no units)
+  const int2 place = p.shares[b];  // (nothing there if the sequence has no units)
   const SeqTokens t = seq_tokens(g, b);
   if (t.bad && threadIdx.x == 0 && hr == 0) raise_flag(g.status, b);
   const int c = r / a.G, hq = h * a.G + (r - c * a.G);
   char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head) * 2;
   float* lse = a.lse ? a.lse + ((int64_t)b * a.heads + hq) * g.C + c : nullptr;
-  const int u = units_of(t);
-  if (u == 0) {
+  const bool any = units_of(t) > 0;
+  if (any && place.y == 1) return;  // written whole
+  if (!any || r >= t.nn * a.G) {
     if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
     if (lse && threadIdx.x == 0) *lse = kNegInf;
     return;
   }
-  const int first = at_first.x, n = at_first.y;
-  if (n == 1) return;  // written whole
-  if (r >= t.nn * a.G) {
-    if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
-    if (lse && threadIdx.x == 0) *lse = kNegInf;
-    return;
-  }
-  const int64_t at = ((int64_t)(first + b) * g.H + h) * a.R + r;  // + share * H * R
+  const int n = place.y;
+  const int64_t at = ((int64_t)(place.x + b) * g.H + h) * a.R + r;  // + share * H * R
   const int64_t step = (int64_t)g.H * a.R;
-  float top = kNegInf;
-  for (int i = lane; i < n; i += 64) top = fmaxf(top, p.part_ml[at + i * step].x);
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) top = fmaxf(top, __shfl_xor(top, m));
-  const float base2 = top == kNegInf ? 0.f : top;
-  float sum = 0.f;
-  for (int i = threadIdx.x; i < n; i += blockDim.x) {
-    const float2 ml = p.part_ml[at + i * step];
-    const float w = exp2_fast(ml.x - base2);
-    s_w[i] = w;
-    sum += w * ml.y;
-  }
-  sum = wave_sum(sum);
-  if (lane == 0) s_sum[wave] = sum;
-  __syncthreads();
-  float o[E];
+  float top = kNegInf, sum = 0.f, o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  const float* po = p.part_o + at * D + lane * E;
-#pragma unroll 8
-  for (int i = wave; i < n; i += waves) {
-    const float w = s_w[i];
-    const float* x = po + i * step * D;
+  for (int i = wave; i < n; i += waves * AHEAD) {
+    float2 ml[AHEAD];
+    float x[AHEAD][E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] += w * x[e];
+    for (int k = 0; k < AHEAD; ++k) {
+      const int64_t from = at + min(i + k * waves, n - 1) * step;
+      ml[k] = p.part_ml[from];
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[k][e] = p.part_o[from * D + lane * E + e];
+    }
+    float grown = top;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (i + k * waves >= n) ml[k].x = kNegInf;  // (past the last: weight 0)
+      grown = fmaxf(grown, ml[k].x);
+    }
+    const float base2 = grown == kNegInf ? 0.f : grown;
+    const float f = exp2_fast(top - base2);
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= f;
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      const float w = exp2_fast(ml[k].x - base2);
+      sum += w * ml[k].y;
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += w * x[k][e];
+    }
+    top = grown;
   }
 #pragma unroll
   for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
-  __syncthreads();
-  sum = 0.f;
-  for (int w = 0; w < waves; ++w) sum += s_sum[w];
-  const bool some = sum != 0.f;
-  if (threadIdx.x < D / 2) {
-    float x = 0.f, y = 0.f;
-    for (int w = 0; w < waves; ++w) {
-      x += s_o[w][2 * threadIdx.x];
-      y += s_o[w][2 * threadIdx.x + 1];
-    }
-    const float inv = 1.f / sum;
-    reinterpret_cast<uint32_t*>(op)[threadIdx.x] = some ? pack_bf16(x * inv, y * inv) : 0u;
+  if (lane == 0) {
+    s_top[wave] = top;
+    s_sum[wave] = sum;
   }
+  __syncthreads();
+  if (threadIdx.x >= D / 2) return;
+  top = kNegInf;
+  for (int w = 0; w < waves; ++w) top = fmaxf(top, s_top[w]);
+  const float base2 = top == kNegInf ? 0.f : top;
+  float x = 0.f, y = 0.f;
+  sum = 0.f;
+  for (int w = 0; w < waves; ++w) {
+    const float f = exp2_fast(s_top[w] - base2);
+    sum += f * s_sum[w];
+    x += f * s_o[w][2 * threadIdx.x];
+    y += f * s_o[w][2 * threadIdx.x + 1];
+  }
+  const bool some = sum != 0.f;
+  const float inv = 1.f / sum;
+  reinterpret_cast<uint32_t*>(op)[threadIdx.x] = some ? pack_bf16(x * inv, y * inv) : 0u;
   if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
@@ -665,7 +652,7 @@ WavePlan wave_plan(int B, int H, int d) {
   p.n_teams = B;
   if (p.split) {
     const int waves = std::max(1, device_cus()) * 4 * (d == 256 ? 1 : kWavesPerSimd);
-    p.n_teams = std::min(kJoinShares, (waves + p.hw * groups - 1) / (p.hw * groups));
+    p.n_teams = std::min(kMaxTeams, (waves + p.hw * groups - 1) / (p.hw * groups));
   }
   p.part_o = nullptr;
   p.part_ml = nullptr;
@@ -673,16 +660,16 @@ WavePlan wave_plan(int B, int H, int d) {
   return p;
 }
 
-template <int D, int NT>
+template <int D>
 hipError_t launch_wave(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
   const dim3 grid = linear_grid(p.n_teams, p.hw * 64, (a.pg.H + p.hw - 1) / p.hw);
   const dim3 block(p.hw * 64);
   if (q4)
-    hipLaunchKernelGGL((k_attend_wave<D, NT, true, false>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, true, false>), grid, block, 0, s, a, p);
   else if ((int64_t)a.pg.B * a.pg.max_tokens * 2 * a.pg.row_bytes > kCacheBytes)
-    hipLaunchKernelGGL((k_attend_wave<D, NT, false, true>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, false, true>), grid, block, 0, s, a, p);
   else
-    hipLaunchKernelGGL((k_attend_wave<D, NT, false, false>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, false, false>), grid, block, 0, s, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
   const int shares = p.n_teams / a.pg.B;  // of a sequence, about
@@ -692,14 +679,6 @@ hipError_t launch_wave(const AttendArgs& a, const WavePlan& p, bool q4, hipStrea
   return hipGetLastError();
 }
 
-template <int D>
-hipError_t launch_tiles(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
-  switch (attend_wave_tiles(a.R)) {
-    case 1: return launch_wave<D, 1>(a, p, q4, s);
-    default: return launch_wave<D, 2>(a, p, q4, s);
-  }
-}
-
 size_t part_ml_bytes(const WavePlan& p, int B, int H, int R) {
   return ((size_t)(p.n_teams + B) * H * R * sizeof(float2) + 255) / 256 * 256;
 }
@@ -707,8 +686,6 @@ size_t part_ml_bytes(const WavePlan& p, int B, int H, int R) {
 constexpr size_t kSharesBytes = kSplitBatch * sizeof(int2);
 
 }  // namespace
-
-int attend_wave_tiles(int R) { return R <= 16 ? 1 : R <= 32 ? 2 : 0; }
 
 size_t attend_wave_workspace(int B, int H, int R, int d) {
   const WavePlan p = wave_plan(B, H, d);
@@ -723,9 +700,9 @@ hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_
     p.part_ml = (float2*)((char*)ws + kSharesBytes);
     p.part_o = (float*)((char*)p.part_ml + part_ml_bytes(p, a.pg.B, a.pg.H, a.R));
   }
-  if (a.pg.d == 64) return launch_tiles<64>(a, p, q4, s);
-  if (a.pg.d == 128) return launch_tiles<128>(a, p, q4, s);
-  return launch_tiles<256>(a, p, q4, s);
+  if (a.pg.d == 64) return launch_wave<64>(a, p, q4, s);
+  if (a.pg.d == 128) return launch_wave<128>(a, p, q4, s);
+  return launch_wave<256>(a, p, q4, s);
 }
 
 }  // namespace epikv

@@ -13,7 +13,7 @@ namespace {
 
 constexpr int kMaxChunk = 1 << 24;
 constexpr int kMaxHeads = 1024;
-constexpr int kMaxTokens = 1 << 28;  // of one sequence: sums over sequences stay in 32 bits
+constexpr int kMaxTokens = 1 << 25;  // of one sequence: sums over sequences stay in 32 bits
 
 int check_rope_cfg(const epikv_rope_cfg* r) {
   if (!r) return EPIKV_EINVAL_NULL;

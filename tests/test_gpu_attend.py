@@ -176,6 +176,40 @@ def test_hidden_slots_hold_anything(E, fmt, C, Hq, H, d):
     check(E, fmt, 2, C, Hq, H, d, 16, n, edit=edit)
 
 
+@pytest.mark.parametrize("C,n", [(1, 40), (1, 5000), (4, 3000), (40, 3000), (200, 300)])
+def test_nan_and_infinity_that_are_seen(E, C, n):
+    """A NaN query, a NaN key, an infinite value and an infinite score reach
+    exactly the rows that the definition lets them reach."""
+    B, Hq, H, d = 4, 4, 2, 128
+    rng = np.random.default_rng(n)
+    c = Cache(E, rng, E.KV_BF16, B, H, d, 16, n)
+    q = rng.standard_normal((B, C, Hq, d))
+    q[0, C - 1, 1, 7] = np.nan
+    kv = rng.standard_normal((B, 2, n, H, d))
+    kv[1, 0, n // 2, 0, 3] = np.nan
+    kv[2, 1, n // 3, 1, 5] = np.inf
+    kv[3, 0, n // 4, 1, 6] = np.inf
+    qd, q64 = bf16(q)
+    held = []
+    for b in range(B):
+        got = []
+        for i in range(2):
+            raw, val = c.encode(kv[b, i])
+            c.fill_rows(b, i, raw)
+            got.append(val)
+        held.append(got)
+    out, lse, _ = run(E, c, C, [n] * B, qd)
+    out = f64(out)
+    for b in range(B):
+        with np.errstate(invalid="ignore", over="ignore"):
+            ro, rl, mag, size = R.attend(q64[b], *held[b], C, d ** -0.5)
+            to, _ = bounds(ro, rl, mag, size, d)
+        assert np.array_equal(np.isnan(out[b]), np.isnan(ro))
+        assert np.array_equal(np.isinf(out[b]), np.isinf(ro))
+        fine = np.isfinite(ro)
+        assert np.all(np.abs(out[b] - ro)[fine] <= to[fine])
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("C", [1, 6, 90])
 def test_pages_out_of_range_are_left_out(E, fmt, C):
