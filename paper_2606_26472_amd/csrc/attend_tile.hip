@@ -478,7 +478,8 @@ TilePlan tile_plan(int B, int H, int R, int d) {
   const int64_t blocks = (int64_t)B * H * p.row_tiles;
   const int64_t want = cus * 8 / p.waves;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, want / blocks));
-  p.paired = p.waves == 4 && p.splits == 1 && B == 1 && blocks <= want;
+  // (rows of 256 channels have one workgroup to a unit, the next when it ends)
+  p.paired = p.waves == 4 && d <= 128 && p.splits == 1 && B == 1 && blocks <= want;
   p.part_o = nullptr;
   p.part_ml = nullptr;
   return p;
