@@ -1,7 +1,7 @@
 """Python binding of libepikv.so (ctypes).
 
-Argument marshalling only: every step of the eviction path runs in the HIP
-kernels behind the C ABI declared in include/epikv.h.  torch tensors supply
+Argument marshalling only: every step of the eviction path, and of filling and
+reading the cache, runs in the HIP kernels behind the C ABI declared in include/epikv.h.  torch tensors supply
 device memory (``data_ptr``) and the current HIP stream.  The library must be
 built (``python -m paper_2606_26472_amd.build``); there is no fallback.
 """
