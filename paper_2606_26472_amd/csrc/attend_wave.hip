@@ -592,7 +592,7 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
     float grown = top;
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      if (i + k * waves >= n) ml[k].x = kNegInf;  // (past the last: weight 0)
+      if (i + k * waves >= n) ml[k].x = kNegInf;  // (past the last)
       grown = fmaxf(grown, ml[k].x);
     }
     const float base2 = grown == kNegInf ? 0.f : grown;
@@ -603,9 +603,11 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       const float w = exp2_fast(ml[k].x - base2);
-      sum += w * ml[k].y;
+      if (i + k * waves < n) {  // (0 times an infinity would not be 0)
+        sum += w * ml[k].y;
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += w * x[k][e];
+        for (int e = 0; e < E; ++e) o[e] += w * x[k][e];
+      }
     }
     top = grown;
   }

@@ -210,6 +210,40 @@ def test_nan_and_infinity_that_are_seen(E, C, n):
         assert np.all(np.abs(out[b] - ro)[fine] <= to[fine])
 
 
+@pytest.mark.parametrize("C,n", [(1, 1), (1, 33), (1, 700), (1, 5000), (1, 40000), (3, 9000),
+                                 (40, 3000)])
+def test_infinite_value_in_the_last_slot(E, C, n):
+    """An infinity stays one however the sequence is cut and joined."""
+    Hq, H, d = 4, 2, 128
+    rng = np.random.default_rng(n)
+    c = Cache(E, rng, E.KV_BF16, 1, H, d, 16, n)
+    q, q64 = bf16(rng.standard_normal((1, C, Hq, d)))
+    kv = rng.standard_normal((2, n, H, d))
+    kv[1, n - 1, 0, 5], kv[1, n - 1, 1, 6] = np.inf, -np.inf
+    held = []
+    for i in range(2):
+        raw, val = c.encode(kv[i])
+        c.fill_rows(0, i, raw)
+        held.append(val)
+    out = f64(run(E, c, C, [n], q)[0])[0]
+    ro, rl, mag, size = R.attend(q64[0], *held, C, d ** -0.5)
+    to, _ = bounds(ro, rl, mag, size, d)
+    fine = np.isfinite(ro)
+    assert np.array_equal(out[~fine], ro[~fine])
+    assert np.all(np.abs(out - ro)[fine] <= to[fine])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("C,heads", [(1, (4, 2, 64)), (3, (8, 2, 128)), (1, (2, 1, 256))])
+def test_batches_past_a_thousand(E, fmt, C, heads):
+    """More sequences than are cut into shares, whose outputs are written
+    without a join."""
+    rng = np.random.default_rng(11)
+    n = rng.integers(0, 60, 1100).tolist()
+    n[5], n[1099] = 0, 400
+    check(E, fmt, 1100, C, *heads, 16, n, [min(x, C) for x in n])
+
+
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("C", [1, 6, 90])
 def test_pages_out_of_range_are_left_out(E, fmt, C):
