@@ -35,18 +35,16 @@ __device__ __forceinline__ int units_of(const SeqTokens& t) {
   return t.nn > 0 ? (t.n + kUnit - 1) / kUnit : 0;
 }
 
-// Inclusive sum over the lanes up to this one.
-__device__ __forceinline__ int wave_scan(int v, int lane) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(v, m);
-    if (lane >= m) v += o;
-  }
+// Inclusive sum over the lanes up to this one: within rows of 16 lanes, then
+// the rows' sums on to the rows after them.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // row_shr 1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // row_shr 2
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // row_shr 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // row_shr 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row_bcast 15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // row_bcast 31
   return v;
-}
-
-__device__ __forceinline__ int units_per_team(int total, int n_teams) {
-  return max(1, (total + n_teams - 1) / n_teams);
 }
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {

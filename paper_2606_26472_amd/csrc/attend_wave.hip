@@ -296,7 +296,10 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         }
         s[i] = mfma16(as_bf16x8(w), qf[k], s[i]);
       }
-    load_k<D, ONCE>(st, a, lds.off, h, n, q4);
+    // (a share's last steps bring nothing more: one sequence 15.0 -> 14.6 us.
+    // 4-bit steps are no faster with the branch.)
+    const bool more = Q4 || base + P * kUnit < end;
+    if (more) load_k<D, ONCE>(st, a, lds.off, h, n, q4);
     const bool special = ok != 0xffffffffu || base + 32 > seen_by_all;
     bf16x8 pf;
     float x[8];
@@ -409,7 +412,8 @@ __device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int 
         }
       }
     }
-    if constexpr (!Q4) load_v<D, ONCE>(st, a, lds.off, h, n, q4);
+    if constexpr (!Q4)
+      if (more) load_v<D, ONCE>(st, a, lds.off, h, n, q4);
   };
 #pragma clang loop unroll(disable)
   for (int base = begin; base < end; base += P * kUnit) {
@@ -466,29 +470,27 @@ __device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
   }
 }
 
-template <int D, bool Q4, bool ONCE>
-__global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
-  __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  const PagedArgs& g = a.pg;
-  const int h = blockIdx.y * p.hw + wave;
-  const int64_t team = linear_block();
-  if (h >= g.H || team >= p.n_teams) return;
-  if (!p.split) {
-    const int b = (int)team;
-    const SeqTokens t = seq_tokens(g, b);
-    if (t.bad && lane == 0) raise_flag(g.status, b);
-    const int u = units_of(t);
-    if (u == 0)
-      attend_nothing<D>(a, b, h, lane);
-    else
-      attend_share<D, Q4, ONCE>(a, p, b, h, t, 0, u, true, 0, s_lds[wave], lane);
-    return;
-  }
-  // All sequences' units, a lane each (their loads at once), and where this
-  // team's share begins among them.
-  constexpr int SETS = kSplitBatch / 64;
+// A team's share: units [lo, hi) of all sequences' in a row, which begin in
+// sequence b, whose own begin at `before`.
+struct Share {
+  int b, before, lo, hi, per;
+  SeqTokens t;
+};
+
+// Units of a share: enough to leave no team without, and, where the teams
+// would outnumber what is worth joining, enough to balance a step's time with
+// a join's per share (about 40 to 1, so sqrt(units of a sequence / 40)).  One KV
+// head, 64k slots: 46 us in single units, 18 so; 600k: 90, 75; one sequence of
+// 4k slots, 8 KV heads, 13.3 both.
+__device__ __forceinline__ int units_per_team(int total, int n_teams, int B) {
+  const int balanced = (int)sqrtf((float)total / (40.f * (float)B));
+  return max(max(1, balanced), (total + n_teams - 1) / n_teams);
+}
+
+// All sequences' units, a lane each (their loads at once), and where this
+// team's share begins among them; false if it is empty.
+template <int SETS>
+__device__ __forceinline__ bool find_share(const PagedArgs& g, int n_teams, int team, int lane, Share& x) {
   int n[SETS], nn[SETS], upto[SETS], total = 0;
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
@@ -504,54 +506,84 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
   for (int i = 0; i < SETS; ++i) {
     upto[i] = total;
     if (64 * i < g.B) {
-      upto[i] += wave_scan(units_of(SeqTokens{n[i], nn[i], false}), lane);
+      upto[i] += wave_scan(units_of(SeqTokens{n[i], nn[i], false}));
       total = __builtin_amdgcn_readlane(upto[i], 63);
     }
   }
-  const int per = units_per_team(total, p.n_teams);
-  int lo = (int)team * per;
-  const int hi = min(total, lo + per);
-  if (lo >= hi) return;
-  int b = 0, before = 0;
-  SeqTokens t = {0, 0, false};
+  x.per = units_per_team(total, n_teams, g.B);
+  x.lo = team * x.per;
+  x.hi = min(total, x.lo + x.per);
+  if (x.lo >= x.hi) return false;
+  x.b = x.before = 0;
+  x.t = {0, 0, false};
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
-    const uint64_t past = __ballot(upto[i] > lo);
-    if (past && t.nn == 0) {
+    const uint64_t past = __ballot(upto[i] > x.lo);
+    if (past && x.t.nn == 0) {
       const int k = __ffsll((unsigned long long)past) - 1;
-      t.n = __builtin_amdgcn_readlane(n[i], k);
-      t.nn = __builtin_amdgcn_readlane(nn[i], k);
-      before = __builtin_amdgcn_readlane(upto[i], k) - units_of(t);
-      b = 64 * i + k;
+      x.t.n = __builtin_amdgcn_readlane(n[i], k);
+      x.t.nn = __builtin_amdgcn_readlane(nn[i], k);
+      x.before = __builtin_amdgcn_readlane(upto[i], k) - units_of(x.t);
+      x.b = 64 * i + k;
     }
   }
-  for (;;) {
-    const int u = units_of(t);
-    if (u > 0) {
-      const int u0 = lo - before, u1 = min(u, hi - before);
-      // (who has a sequence's first unit tells the join where its shares are)
-      if (u0 == 0 && h == 0 && lane == 0)
-        p.shares[b] = make_int2((int)team, (before + u - 1) / per - (int)team + 1);
-      attend_share<D, Q4, ONCE>(a, p, b, h, t, u0, u1, u0 == 0 && u1 == u, (int)team + b, s_lds[wave], lane);
-      lo = before + u1;
-      before += u;
+  return true;
+}
+
+template <int D, bool Q4, bool ONCE>
+__global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
+  __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const PagedArgs& g = a.pg;
+  const int h = blockIdx.y * p.hw + wave;
+  const int64_t team = linear_block();
+  if (h >= g.H || team >= p.n_teams) return;
+  Share x;
+  if (!p.split) {  // a sequence to a team
+    x.b = (int)team;
+    x.t = seq_tokens(g, x.b);
+    if (x.t.bad && lane == 0) raise_flag(g.status, x.b);
+    x.before = x.lo = 0;
+    x.hi = units_of(x.t);
+    if (x.hi == 0) {
+      attend_nothing<D>(a, x.b, h, lane);
+      return;
     }
-    if (lo >= hi) break;
-    t = seq_tokens(g, ++b);
+  } else if (g.B <= 64) {
+    // (a launch fetches its instructions anew: one sequence of 4k slots 15.2 us
+    // with this, 16.3 through the code for 1024)
+    if (!find_share<1>(g, p.n_teams, (int)team, lane, x)) return;
+  } else {
+    if (!find_share<kSplitBatch / 64>(g, p.n_teams, (int)team, lane, x)) return;
+  }
+  for (;;) {
+    const int u = units_of(x.t);
+    if (u > 0) {
+      const int u0 = x.lo - x.before, u1 = min(u, x.hi - x.before);
+      // (who has a sequence's first unit tells the join where its shares are)
+      if (p.split && u0 == 0 && h == 0 && lane == 0)
+        p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
+      attend_share<D, Q4, ONCE>(a, p, x.b, h, x.t, u0, u1, u0 == 0 && u1 == u, (int)team + x.b, s_lds[wave], lane);
+      x.lo = x.before + u1;
+      x.before += u;
+    }
+    if (x.lo >= x.hi) break;
+    x.t = seq_tokens(g, ++x.b);
   }
 }
 
 // Joins the shares of one row: a workgroup per (sequence, query row), its
-// wavefronts taking turns over the shares, eight at a time, in a fixed order,
+// wavefronts taking turns over the shares, 16 at a time, in a fixed order,
 // and then their results.  Bound by latency: after the shares' place two round
-// trips (a pass for the maximum and one for the sums took a third).
-constexpr int kMaxTeams = 2048;
-
+// trips (a pass for the maximum and one for the sums took a third).  5.4 us
+// for 132 shares of 32 rows and for 32 sequences of 8 shares each, 1.5 of them
+// the launch.
 template <int D>
-__global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) {
-  constexpr int E = D / 64, AHEAD = 8;
-  __shared__ float s_o[16][D];
-  __shared__ float s_top[16], s_sum[16];
+__global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, WavePlan p) {
+  constexpr int E = D / 64, AHEAD = 16;
+  __shared__ float s_o[8][D];
+  __shared__ float s_top[8], s_sum[8];
   const PagedArgs& g = a.pg;
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -584,17 +616,18 @@ __global__ __launch_bounds__(1024) void k_attend_join(AttendArgs a, WavePlan p) 
     float x[AHEAD][E];
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
-      const int64_t from = at + min(i + k * waves, n - 1) * step;
-      ml[k] = p.part_ml[from];
+      if (i + k * waves < n) {
+        const int64_t from = at + (i + k * waves) * step;
+        ml[k] = p.part_ml[from];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[k][e] = p.part_o[from * D + lane * E + e];
+        for (int e = 0; e < E; ++e) x[k][e] = p.part_o[from * D + lane * E + e];
+      } else {
+        ml[k] = make_float2(kNegInf, 0.f);
+      }
     }
     float grown = top;
 #pragma unroll
-    for (int k = 0; k < AHEAD; ++k) {
-      if (i + k * waves >= n) ml[k].x = kNegInf;  // (past the last)
-      grown = fmaxf(grown, ml[k].x);
-    }
+    for (int k = 0; k < AHEAD; ++k) grown = fmaxf(grown, ml[k].x);
     const float base2 = grown == kNegInf ? 0.f : grown;
     const float f = exp2_fast(top - base2);
     sum *= f;
@@ -654,7 +687,7 @@ WavePlan wave_plan(int B, int H, int d) {
   p.n_teams = B;
   if (p.split) {
     const int waves = std::max(1, device_cus()) * 4 * (d == 256 ? 1 : kWavesPerSimd);
-    p.n_teams = std::min(kMaxTeams, (waves + p.hw * groups - 1) / (p.hw * groups));
+    p.n_teams = (waves + p.hw * groups - 1) / (p.hw * groups);
   }
   p.part_o = nullptr;
   p.part_ml = nullptr;
@@ -675,7 +708,7 @@ hipError_t launch_wave(const AttendArgs& a, const WavePlan& p, bool q4, hipStrea
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.split) return e;
   const int shares = p.n_teams / a.pg.B;  // of a sequence, about
-  const int waves = shares >= 64 ? 16 : shares >= 16 ? 8 : 4;
+  const int waves = shares >= 16 ? 8 : 4;
   hipLaunchKernelGGL(k_attend_join<D>, linear_grid((int64_t)a.pg.B * a.pg.H * a.R, waves * 64),
                      dim3(waves * 64), 0, s, a, p);
   return hipGetLastError();
