@@ -495,12 +495,9 @@ __device__ __forceinline__ bool find_share(const PagedArgs& g, int n_teams, int 
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {
     const int b = 64 * i + lane;
-    n[i] = nn[i] = 0;
-    if (b < g.B) {
-      const SeqTokens t = seq_tokens(g, b);
-      n[i] = t.n;
-      nn[i] = t.nn;
-    }
+    const SeqTokens t = seq_tokens(g, min(b, g.B - 1));  // (no branch between the loads)
+    n[i] = b < g.B ? t.n : 0;
+    nn[i] = b < g.B ? t.nn : 0;
   }
 #pragma unroll
   for (int i = 0; i < SETS; ++i) {

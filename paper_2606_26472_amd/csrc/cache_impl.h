@@ -20,7 +20,8 @@ struct SeqTokens {
 __device__ __forceinline__ SeqTokens seq_tokens(const PagedArgs& a, int b) {
   SeqTokens t;
   t.n = a.n_cached[b];
-  t.nn = a.n_new ? a.n_new[b] : a.C;
+  const int given = (a.n_new ? a.n_new : a.n_cached)[b];  // (no branch between two loads)
+  t.nn = a.n_new ? given : a.C;
   t.bad = t.nn < 0 || t.nn > a.C || t.n < t.nn || t.n > a.max_tokens;
   if (t.bad) t.n = t.nn = 0;
   return t;
