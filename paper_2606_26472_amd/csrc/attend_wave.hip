@@ -6,8 +6,13 @@
 // already laid out as the second operand of O^T = V^T P^T: with v_mfma
 // 16x16x32, lane (n, g) = (lane % 16, lane / 16) gets the scores of query row
 // n against tokens 4g .. 4g+3 of each 16-token tile, and 32 tokens make its 8
-// values of the second product.  Nothing passes through LDS but row addresses,
-// and the running maximum's growth is the only exchange between lanes.
+// values of the second product.  Nothing passes through LDS but row addresses
+// (and 4-bit values and scales), and the running maximum's growth is the only
+// exchange between lanes.
+//
+// Bound by HBM: 32 sequences of 8k-32k tokens (8 KV heads of 128, 4 query heads
+// each) 2.69 GB in 406 us, 6.6 TB/s; in 4 bits 0.72 GB in 138 us, 5.2 TB/s, with
+// the vector units busy 45 % of the time.  One sequence of 4k: 8 us, latency.
 #include "attend_impl.h"
 
 namespace epikv {

@@ -7,7 +7,8 @@ namespace {
 
 // One thread per (position, pair): the pair's frequency, its angle, cosine
 // and sine in 64 bits (an angle of 2^24 radians keeps 28 bits after the
-// point), rounded to float32 once.
+// point), rounded to float32 once.  Bound by the 64-bit functions: 131072
+// positions of 64 pairs 87 us, once for a model.
 __global__ __launch_bounds__(256) void k_rope_table(RopeTableArgs a) {
   const int64_t t = linear_block() * 256 + threadIdx.x;
   if (t >= (int64_t)a.n_pos * a.half) return;
