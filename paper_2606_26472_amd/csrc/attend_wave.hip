@@ -671,11 +671,12 @@ __global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, WavePlan p) {
   if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
-// bf16 rows are not kept in the caches when the page tables cover more than the
-// last-level cache holds: 32 sequences of 8k-32k tokens 453 -> 415 us.  Fewer
-// may still be there at the next token: 4224 slots 16.7 us kept, 18.5 not.
+// bf16 rows are not kept in the caches when the page tables cover more than half
+// of the last-level cache: 32 sequences of 8k-32k tokens 453 -> 415 us, 4 of 16k
+// (256 MiB) 55.2 -> 50.7.  Fewer may still be there at the next token: 2 of 16k
+// 29.5 us kept, 32.0 not; 4224 slots 16.7, 18.5.
 // (4-bit rows share lines between wavefronts and are kept: no difference.)
-constexpr int64_t kCacheBytes = 256 << 20;
+constexpr int64_t kCacheBytes = 128 << 20;
 
 // Wavefronts resident per SIMD that the shares are counted for.
 constexpr int kWavesPerSimd = 2;
