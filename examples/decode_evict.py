@@ -29,15 +29,25 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2606_26472_amd import epikv as E  # noqa: E402
 
 
+def check_positions(prompt, tokens, max_positions):
+    """A token past the table would be left out of the cache."""
+    if prompt + tokens > max_positions:
+        raise ValueError(f"{prompt} + {tokens} tokens, the positions' table holds {max_positions}")
+
+
 class Decoder:
     """The loop's state: weights, cache, page table, lengths, scores."""
 
     def __init__(self, batch=4, layers=4, hidden=1024, heads=8, kv_heads=2, head_dim=128, page=16, prompt=100,
                  budget=256, every=64, fmt="bf16", theta=500000.0, max_positions=4096, seed=0, history=False):
+        if layers < 2:
+            raise ValueError("the scores need two layers at least, one of each band")
+        if not 1 <= prompt <= max_positions:
+            raise ValueError(f"a prompt of 1 to {max_positions} tokens (the positions' table)")
         dev = self.dev = torch.device("cuda")
         g = self.gen = torch.Generator(device=dev).manual_seed(seed)
         self.B, self.L, self.D, self.Hq, self.H, self.d = batch, layers, hidden, heads, kv_heads, head_dim
-        self.prompt, self.every = prompt, every
+        self.prompt, self.every, self.max_positions = prompt, every, max_positions
         self.cfg = E.default_cfg(batch=batch, hidden=hidden, n_layers=layers, n_kv_heads=kv_heads,
                                  head_dim=head_dim, page_size=page, n_band_a=1, n_band_b=1, budget=budget,
                                  kv_format=E.KV_MXFP4 if fmt == "mxfp4" else E.KV_BF16)
@@ -122,6 +132,7 @@ class Decoder:
         self.n_cached.copy_(self.n_keep)
 
     def run(self, n_tokens):
+        check_positions(self.prompt, self.tokens + n_tokens, self.max_positions)
         def embed(n):
             return torch.randn(self.B, n, self.D, generator=self.gen, device=self.dev).bfloat16()
         if self.tokens == 0:
@@ -143,9 +154,13 @@ def main(argv=None):
     p.add_argument("--tokens", type=int, default=512)
     p.add_argument("--budget", type=int, default=256)
     p.add_argument("--every", type=int, default=64)
+    p.add_argument("--max-positions", type=int, default=4096)
     a = p.parse_args(argv)
-    m = Decoder(batch=a.batch, layers=a.layers, prompt=a.prompt, budget=a.budget, every=a.every, fmt=a.format)
-    m.run(min(a.tokens, a.every))  # (warm)
+    warm = min(a.tokens, a.every)
+    check_positions(a.prompt, warm + a.tokens, a.max_positions)
+    m = Decoder(batch=a.batch, layers=a.layers, prompt=a.prompt, budget=a.budget, every=a.every, fmt=a.format,
+                max_positions=a.max_positions)
+    m.run(warm)
     torch.cuda.synchronize()
     start = time.perf_counter()
     m.run(a.tokens)

@@ -378,11 +378,21 @@ def _address(arr):
     return None if arr is None else arr.buffer_info()[0]
 
 
+def _every_layer(cfg: Cfg, arr, where):
+    """The library reads one address per band layer from the host array."""
+    if arr is None or cfg.signal != SIGNAL_HS:
+        return
+    want = cfg.n_band_a + cfg.n_band_b
+    if len(arr) < want:
+        raise ValueError(f"{where}: hidden states of {len(arr)} layers, cfg has {want} band layers")
+
+
 def epikv_score(cfg: Cfg, chunk: int, hidden=None, ld_tok=0, ld_seq=0,
                 pool: Pool | None = None, page_table=None, ld_pt=0,
                 n_cached=None, state_in=None, state_out=None, sig=None,
                 workspace=None, workspace_bytes_=0, stream=None):
     arr = _hidden_array(hidden)
+    _every_layer(cfg, arr, "epikv_score")
     _check(lib().epikv_score(
         ctypes.byref(cfg), int(chunk), _address(arr), int(ld_tok), int(ld_seq),
         ctypes.byref(pool) if pool is not None else None, _ptr(page_table),
@@ -403,6 +413,7 @@ def epikv_zscore(cfg: Cfg, chunk: int, sig, n_cached, state_in, state_out,
 def epikv_score_tokens(cfg: Cfg, chunk: int, hidden, ld_tok, ld_seq, n_cached,
                        state_in, state_out, scores, ld_s, stream=None):
     arr = _hidden_array(hidden)
+    _every_layer(cfg, arr, "epikv_score_tokens")
     _check(lib().epikv_score_tokens(
         ctypes.byref(cfg), int(chunk), _address(arr), int(ld_tok), int(ld_seq),
         _ptr(n_cached), _ptr(state_in), _ptr(state_out), _ptr(scores),
@@ -499,7 +510,13 @@ def make_step_io(chunk, hidden, ld_tok, ld_seq, n_cached, n_prefix,
     return io
 
 
+def _step_layers(cfg: Cfg, io: StepIO, where):
+    if io.chunk > 0:  # (a step without new tokens reads no hidden states)
+        _every_layer(cfg, getattr(io, "_hidden_keepalive", None), where)
+
+
 def epikv_evict_step(cfg: Cfg, io: StepIO, stream=None):
+    _step_layers(cfg, io, "epikv_evict_step")
     _check(lib().epikv_evict_step(ctypes.byref(cfg), ctypes.byref(io),
                                   _stream(stream)), "epikv_evict_step")
 
@@ -507,6 +524,7 @@ def epikv_evict_step(cfg: Cfg, io: StepIO, stream=None):
 def epikv_evict_step_noalloc(cfg: Cfg, io: StepIO, stream=None):
     """epikv_evict_step with the library's per-GPU scratch array
     (io.workspace is ignored)."""
+    _step_layers(cfg, io, "epikv_evict_step_noalloc")
     _check(lib().epikv_evict_step_noalloc(ctypes.byref(cfg), ctypes.byref(io),
                                           _stream(stream)),
            "epikv_evict_step_noalloc")
