@@ -649,7 +649,9 @@ int epikv_rope_table(const epikv_rope_cfg* rope, float* table, hipStream_t strea
  * gradient of the output (and, for amplitude 1, the inverse).
  * head_dim a multiple of 16 from 16 to 1024, rotary_dim <= head_dim; dtype
  * of x and y an epikv_dtype.  y may be x (same base and strides); any other
- * overlap of the two is EPIKV_EALIAS.
+ * overlap of the two is EPIKV_EALIAS.  (Here and below, rows that lie between
+ * each other's without sharing an element, as heads of one fused projection
+ * do, do not overlap.)
  * positions: int32, ld_pos = 0: [batch], the position of the sequence's
  * first token, the rest follow; else [batch][ld_pos >= chunk], one a token.
  * Tokens whose position is out of range are not written (and flagged).
@@ -694,7 +696,9 @@ typedef struct epikv_append_io {
  * -126 at least; its values round to the nearest code, ties to the even one.
  * A block with a NaN or an infinity reads back as NaN.
  * Queries of padding tokens (c >= n_new[b]) and of positions out of range are
- * not written.  k and v must not overlap the pool (not checked).
+ * not written.  q_out may be q; any other overlap with q, and any with k or v,
+ * is EPIKV_EALIAS (the launch reads those while it writes the queries).  k and
+ * v must not overlap the pool (not checked).
  * Pages of different sequences may be shared only where neither appends.
  */
 int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io, hipStream_t stream);
@@ -756,7 +760,7 @@ size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t
  * has out 0 and lse -infinity.  Slots a token does not see, whatever they
  * hold, do not reach its result.
  * The cache is not written, so tokens must be appended before; out may not
- * overlap q (EPIKV_EALIAS, checked on their whole spans).  The workspace
+ * overlap q (EPIKV_EALIAS).  The workspace
  * (16-byte aligned, any contents) must overlap no other argument; calls that
  * share one must not overlap in time.  May be captured in a HIP graph.
  */

@@ -80,13 +80,40 @@ bool same_rows(const epikv_rows* x, const epikv_rows* y) {
          x->ld_head == y->ld_head;
 }
 
+// Whether an element of x (hx heads) may be one of y (hy heads).  Spans that
+// overlap may still hold rows between each other's, as slices of one fused
+// projection do: by the remainders of a period P, which every stride that is a
+// multiple of P leaves as they are, x has [0, wx) and y [at, at + wy).  The
+// periods tried are the strides.
+bool rows_meet(const epikv_rows* x, int hx, const epikv_rows* y, int hy, int B, int C, int d, int es) {
+  if (!overlap(x->base, rows_span(x, B, C, hx, d, es), y->base, rows_span(y, B, C, hy, d, es)))
+    return false;
+  struct Axis {
+    int64_t stride, n;
+  };
+  const Axis ax[3] = {{x->ld_seq, B}, {x->ld_tok, C}, {x->ld_head, hx}};
+  const Axis ay[3] = {{y->ld_seq, B}, {y->ld_tok, C}, {y->ld_head, hy}};
+  const int64_t between = (int64_t)((uintptr_t)y->base - (uintptr_t)x->base) / es;
+  auto width = [&](const Axis* a, int64_t period) {
+    int64_t w = d;
+    for (int i = 0; i < 3; ++i)
+      if (a[i].n > 1 && a[i].stride % period) w += (a[i].n - 1) * a[i].stride;
+    return w;
+  };
+  for (const Axis* a : {ax, ay})
+    for (int i = 0; i < 3; ++i) {
+      const int64_t period = a[i].stride;
+      if (a[i].n == 1 || period == 0) continue;
+      const int64_t at = (between % period + period) % period;
+      if (at >= width(ax, period) && at + width(ay, period) <= period) return false;
+    }
+  return true;
+}
+
 // y may be x itself or lie apart from it.
 int check_alias(const epikv_rows* x, const epikv_rows* y, int B, int C, int heads, int d, int es) {
   if (same_rows(x, y)) return EPIKV_OK;
-  return overlap(x->base, rows_span(x, B, C, heads, d, es), y->base,
-                 rows_span(y, B, C, heads, d, es))
-             ? EPIKV_EALIAS
-             : EPIKV_OK;
+  return rows_meet(x, heads, y, heads, B, C, d, es) ? EPIKV_EALIAS : EPIKV_OK;
 }
 
 int check_positions(const int32_t* positions, int64_t ld_pos, int32_t chunk) {
@@ -272,11 +299,9 @@ EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
     if (st) return st;
     st = check_alias(&io->q, &io->q_out, B, C, io->n_heads, d, 2);
     if (st) return st;
-    // (the launch reads keys and values while it writes the queries)
-    const size_t nq = rows_span(&io->q_out, B, C, io->n_heads, d, 2);
-    if (!same_rows(&io->q, &io->q_out) &&
-        (overlap(io->q_out.base, nq, io->k.base, rows_span(&io->k, B, C, H, d, 2)) ||
-         overlap(io->q_out.base, nq, io->v.base, rows_span(&io->v, B, C, H, d, 2))))
+    // (the launch reads keys and values while it writes the queries, in place or not)
+    if (rows_meet(&io->q_out, io->n_heads, &io->k, H, B, C, d, 2) ||
+        rows_meet(&io->q_out, io->n_heads, &io->v, H, B, C, d, 2))
       return EPIKV_EALIAS;
   }
   if (!append_fits((int64_t)B * C, H, io->q.base ? io->n_heads : 0, d)) return EPIKV_EINVAL_SHAPE;
@@ -307,10 +332,7 @@ EPIKV_EXPORT int epikv_read(const epikv_cfg* cfg, const epikv_read_io* io, hipSt
     st = x->base ? check_out_rows(x, B, C, H, d) : EPIKV_OK;
     if (st) return st;
   }
-  if (io->k.base && io->v.base &&
-      overlap(io->k.base, rows_span(&io->k, B, C, H, d, 2), io->v.base,
-              rows_span(&io->v, B, C, H, d, 2)))
-    return EPIKV_EALIAS;
+  if (io->k.base && io->v.base && rows_meet(&io->k, H, &io->v, H, B, C, d, 2)) return EPIKV_EALIAS;
   if (!append_fits((int64_t)B * C, H, 0, d)) return EPIKV_EINVAL_SHAPE;
   ReadArgs a;
   a.pg = paged_args(cfg, &io->pool, io->layer, C, io->page_table, io->ld_pt, io->first, nullptr,
@@ -341,9 +363,9 @@ EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
   if (st) return st;
   st = check_out_rows(&io->out, B, C, io->n_heads, d);
   if (st) return st;
+  if (rows_meet(&io->out, io->n_heads, &io->q, io->n_heads, B, C, d, 2)) return EPIKV_EALIAS;
   const size_t n_out = rows_span(&io->out, B, C, io->n_heads, d, 2);
   const size_t n_q = rows_span(&io->q, B, C, io->n_heads, d, 2);
-  if (overlap(io->out.base, n_out, io->q.base, n_q)) return EPIKV_EALIAS;
   const size_t need = attend_workspace(B, C, H, io->n_heads, d);
   if (need) {
     if (!io->workspace || io->workspace_bytes < need) return EPIKV_EWORKSPACE;
