@@ -569,8 +569,9 @@ int epikv_evict_step_noalloc(const epikv_cfg* cfg, const epikv_step_io* io,
  * [n_new[b], min(ld_pt*page_size, 2^25)] (the sequence counts as having no
  * tokens), a
  * page id outside [0, n_pages) (its tokens are neither written nor read, and
- * attention leaves them out) and a position outside [0, n_pos) (the token is
- * left out).
+ * attention leaves them out), a position outside [0, n_pos) (the token is
+ * left out) and a slot past the row that takes token ids (the id is not
+ * written).
  */
 
 /*
@@ -680,7 +681,9 @@ typedef struct epikv_append_io {
   epikv_rows q, q_out;          /* optional: bf16 queries, rotated into q_out
                                    (which may be q) in the same launch */
   int32_t* pos;                 /* optional [B][ld_s]: pos[b][slot] = the
-                                   token's position, the ids the step moves */
+                                   token's position, the ids the step moves;
+                                   a token with slot >= ld_s is appended
+                                   without one, and flags its sequence */
   int64_t ld_s;
   int32_t* seq_status;          /* optional [B] */
 } epikv_append_io;

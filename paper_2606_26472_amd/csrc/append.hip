@@ -56,8 +56,12 @@ __device__ __forceinline__ void append_vecs(const AppendArgs& a, int b, int c, i
     raise_flag(g.status, b);
     return;
   }
-  if (kv == 0 && h == 0 && vec == 0 && a.pos && slot < a.ld_s)
-    a.pos[(int64_t)b * a.ld_s + slot] = (int32_t)p;
+  if (kv == 0 && h == 0 && vec == 0 && a.pos) {
+    if (slot < a.ld_s)
+      a.pos[(int64_t)b * a.ld_s + slot] = (int32_t)p;
+    else
+      raise_flag(g.status, b);  // (no place for its id: a step would move one that was never set)
+  }
   f32x4 cs[4];
   if (rot) {
     const f32x4* t4 = reinterpret_cast<const f32x4*>(a.rope.table + p * (r / 2) + (half ? first * 8 : vec * 4));
