@@ -545,6 +545,49 @@ def _expect(t, dtype, shape, what):
         raise ValueError(f"{what}: shape {tuple(shape)} expected, got {tuple(t.shape)}")
 
 
+_int32 = _float32 = None  # torch's, once a tensor has been looked at
+
+
+def _rows_held(t, ld, what, floats=False):
+    """How many rows, ld entries apart, a tensor of int32 (or float32) holds
+    (the kernels read them by its address); an address is taken as it is."""
+    if t is None or isinstance(t, int):
+        return 1 << 62
+    global _int32, _float32
+    if _int32 is None:
+        import torch
+        _int32, _float32 = torch.int32, torch.float32
+    want = _float32 if floats else _int32
+    if t.dtype != want:
+        raise ValueError(f"{what}: {want} expected, got {t.dtype}")
+    if t.is_contiguous() and (t.dim() != 2 or t.shape[0] != 1):
+        return t.numel() // ld
+    if t.dim() == 2 and (t.shape[0] == 1 or t.stride(0) == ld) and (t.shape[1] == 1 or t.stride(1) == 1):
+        # (part of a wider one: its rows end where the storage does)
+        return (t.untyped_storage().nbytes() // 4 - t.storage_offset()) // ld
+    raise ValueError(f"{what}: adjacent entries, rows {ld} apart, expected")
+
+
+def _expect_rows(t, rows, ld, what, floats=False):
+    have = _rows_held(t, ld, what, floats)
+    if have < rows:
+        raise ValueError(f"{what}: holds {have} rows of {ld}, {rows} needed")
+
+
+def _expect_table(rope: Rope, table):
+    _expect_rows(table, rope.n_pos * rope.rotary_dim, 1, "table", True)
+
+
+def _dims_held(dims, **tensors):
+    """What a cfg has to have (the batch first), or, where a tensor (given
+    with its entries a sequence) holds fewer sequences, what none has."""
+    for what, (t, ld) in tensors.items():
+        have = _rows_held(t, max(1, int(ld)), what)
+        if have < dims[0]:
+            return dims + (f"{what} for {have} sequences only",)
+    return dims
+
+
 def _same_shape(cfg: Cfg, io, where):
     if io._dims != (cfg.batch, cfg.n_kv_heads, cfg.head_dim):
         raise ValueError(f"{where}: built for (batch, n_kv_heads, head_dim) = {io._dims}, "
@@ -568,10 +611,25 @@ def epikv_rope(rope: Rope, table, dtype, batch, chunk, n_heads, head_dim, x,
                y, positions, ld_pos=0, transpose=False, seq_status=None,
                stream=None):
     """x and y: tensors [batch][chunk][n_heads][head_dim], or Rows."""
-    xr, yr = _as_rows(x), _as_rows(y)
-    for t, what in ((x, "x"), (y, "y")):
-        _expect(t, "float32" if dtype == DTYPE_FP32 else "bfloat16",
-                (batch, chunk, n_heads, head_dim), what)
+    # (this call's time is the host's for a token a sequence: no more than needed)
+    if x.__class__ is Rows and y.__class__ is Rows:
+        xr, yr = x, y
+    else:
+        for t, what in ((x, "x"), (y, "y")):
+            _expect(t, "float32" if dtype == DTYPE_FP32 else "bfloat16",
+                    (batch, chunk, n_heads, head_dim), what)
+        xr, yr = _as_rows(x), _as_rows(y)
+    try:
+        enough = (table.nbytes >= 4 * rope.n_pos * rope.rotary_dim and table.dtype is _float32
+                  and positions.nbytes >= 4 * batch * (ld_pos or 1) and positions.dtype is _int32
+                  and table.is_contiguous() and positions.is_contiguous())
+    except AttributeError:  # (addresses)
+        enough = False
+    if not enough:
+        _expect_table(rope, table)
+        _expect_rows(positions, batch, ld_pos or 1, "positions")
+    if seq_status is not None:
+        _expect_rows(seq_status, batch, 1, "seq_status")
     _check(lib().epikv_rope(
         ctypes.byref(rope), _ptr(table), int(dtype), int(batch), int(chunk),
         int(n_heads), int(head_dim), ctypes.byref(xr), ctypes.byref(yr),
@@ -591,8 +649,12 @@ def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
     _expect(k, "bfloat16", (k.shape[0], int(chunk)) + tuple(k.shape[2:]), "k")
     if q is not None:
         _expect(q, "bfloat16", (k.shape[0], int(chunk), q.shape[2], k.shape[3]), "q")
+    if rope is not None:
+        _expect_table(rope, table)
     io = AppendIO()
-    io._dims = (k.shape[0], k.shape[2], k.shape[3])
+    io._dims = _dims_held((k.shape[0], k.shape[2], k.shape[3]), page_table=(page_table, ld_pt),
+                          n_cached=(n_cached, 1), n_new=(n_new, 1), positions=(positions, ld_pos),
+                          pos=(pos, ld_s), seq_status=(seq_status, 1))
     io._keepalive = [page_table, n_cached, n_new, k, v, rope, table, positions,
                      q, q_out, pos, seq_status]
     io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
@@ -620,7 +682,8 @@ def make_read_io(chunk, pool: Pool, layer, page_table, ld_pt, first, k=None,
     for t, what in ((k, "k"), (v, "v")):
         _expect(t, "bfloat16", (like.shape[0], int(chunk)) + tuple(like.shape[2:]), what)
     io = ReadIO()
-    io._dims = (like.shape[0], like.shape[2], like.shape[3])
+    io._dims = _dims_held((like.shape[0], like.shape[2], like.shape[3]), page_table=(page_table, ld_pt),
+                          first=(first, 1), seq_status=(seq_status, 1))
     io._keepalive = [page_table, first, k, v, seq_status]
     io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
     io.page_table, io.ld_pt, io.first = _ptr(page_table), int(ld_pt), _ptr(first)
@@ -647,7 +710,8 @@ def make_attend_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, q, out
         if not lse.is_contiguous():
             raise ValueError("lse must be contiguous")
     io = AttendIO()
-    io._dims = (B, d)
+    io._dims = _dims_held((B, d), page_table=(page_table, ld_pt), n_cached=(n_cached, 1), n_new=(n_new, 1),
+                          seq_status=(seq_status, 1))
     io._keepalive = [page_table, n_cached, n_new, q, out, lse, seq_status, workspace]
     io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
     io.page_table, io.ld_pt = _ptr(page_table), int(ld_pt)
