@@ -13,6 +13,8 @@
 // Bound by HBM: 32 sequences of 8k-32k tokens (8 KV heads of 128, 4 query heads
 // each) 2.69 GB in 406 us, 6.6 TB/s; in 4 bits 0.72 GB in 138 us, 5.2 TB/s, with
 // the vector units busy 45 % of the time.  One sequence of 4k: 8 us, latency.
+#include <type_traits>
+
 #include "attend_impl.h"
 
 namespace epikv {
@@ -188,7 +190,7 @@ constexpr int steps_ahead() {
 // Units [u0, u1) of sequence b for KV head h.  whole: the units are all of the
 // sequence's, the result is final; else it goes to partial slot `slot`.
 template <int D, bool Q4, bool ONCE>
-__device__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
+__device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
                              int u0, int u1, bool whole, int slot, Scratch<D, Q4>& lds, int lane) {
   using S = Step<D, Q4>;
   constexpr int KS = S::KS, VC = D / 16;
@@ -475,10 +477,10 @@ __device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
   }
 }
 
-// A team's share: units [lo, hi) of all sequences' in a row, which begin in
-// sequence b, whose own begin at `before`.
+// A team's share: units [lo, hi) of all sequences' in a row (`total` of them),
+// which begin in sequence b, whose own begin at `before`.
 struct Share {
-  int b, before, lo, hi, per;
+  int b, before, lo, hi, per, total;
   SeqTokens t;
 };
 
@@ -512,6 +514,7 @@ __device__ __forceinline__ bool find_share(const PagedArgs& g, int n_teams, int 
       total = __builtin_amdgcn_readlane(upto[i], 63);
     }
   }
+  x.total = total;
   x.per = units_per_team(total, n_teams, g.B);
   x.lo = team * x.per;
   x.hi = min(total, x.lo + x.per);
@@ -532,7 +535,16 @@ __device__ __forceinline__ bool find_share(const PagedArgs& g, int n_teams, int 
   return true;
 }
 
-template <int D, bool Q4, bool ONCE>
+// bf16 rows are not kept in the caches when the sequences hold more than half
+// of the last-level cache: 32 sequences of 8k-32k tokens 453 -> 415 us, 4 of 16k
+// (256 MiB) 55.2 -> 50.7.  Fewer may still be there at the next token: 2 of 16k
+// 29.0 us kept, 31.0 not; 4224 slots 13.3, 14.5; 32 of 1024 29.3, 31.8.
+// (4-bit rows share lines between wavefronts and are kept: no difference.)
+constexpr int64_t kCacheBytes = 128 << 20;
+
+// LARGE: the page tables cover more than that; whether the sequences hold as
+// much, their counts say.
+template <int D, bool Q4, bool LARGE>
 __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
   __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -559,20 +571,32 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
   } else {
     if (!find_share<kSplitBatch / 64>(g, p.n_teams, (int)team, lane, x)) return;
   }
-  for (;;) {
-    const int u = units_of(x.t);
-    if (u > 0) {
-      const int u0 = x.lo - x.before, u1 = min(u, x.hi - x.before);
-      // (who has a sequence's first unit tells the join where its shares are)
-      if (p.split && u0 == 0 && h == 0 && lane == 0)
-        p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
-      attend_share<D, Q4, ONCE>(a, p, x.b, h, x.t, u0, u1, u0 == 0 && u1 == u, (int)team + x.b, s_lds[wave], lane);
-      x.lo = x.before + u1;
-      x.before += u;
+  auto walk = [&](auto once) {
+    for (;;) {
+      const int u = units_of(x.t);
+      if (u > 0) {
+        const int u0 = x.lo - x.before, u1 = min(u, x.hi - x.before);
+        // (who has a sequence's first unit tells the join where its shares are)
+        if (p.split && u0 == 0 && h == 0 && lane == 0)
+          p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
+        attend_share<D, Q4, decltype(once)::value>(a, p, x.b, h, x.t, u0, u1, u0 == 0 && u1 == u,
+                                                   (int)team + x.b, s_lds[wave], lane);
+        x.lo = x.before + u1;
+        x.before += u;
+      }
+      if (x.lo >= x.hi) break;
+      x.t = seq_tokens(g, ++x.b);
     }
-    if (x.lo >= x.hi) break;
-    x.t = seq_tokens(g, ++x.b);
+  };
+  if constexpr (LARGE) {
+    // (without shares a team knows one sequence of more than a thousand: too
+    // many to be there at the next token, unless all are short)
+    if (!p.split || (int64_t)x.total * (2 * kUnit) * g.row_bytes > kCacheBytes) {
+      walk(std::true_type{});
+      return;
+    }
   }
+  walk(std::false_type{});
 }
 
 // Joins the shares of one row: a workgroup per (sequence, query row), its
@@ -670,13 +694,6 @@ __global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, WavePlan p) {
   reinterpret_cast<uint32_t*>(op)[threadIdx.x] = some ? pack_bf16(x * inv, y * inv) : 0u;
   if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
-
-// bf16 rows are not kept in the caches when the page tables cover more than half
-// of the last-level cache: 32 sequences of 8k-32k tokens 453 -> 415 us, 4 of 16k
-// (256 MiB) 55.2 -> 50.7.  Fewer may still be there at the next token: 2 of 16k
-// 29.5 us kept, 32.0 not; 4224 slots 16.7, 18.5.
-// (4-bit rows share lines between wavefronts and are kept: no difference.)
-constexpr int64_t kCacheBytes = 128 << 20;
 
 // Wavefronts resident per SIMD that the shares are counted for.
 constexpr int kWavesPerSimd = 2;
