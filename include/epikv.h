@@ -187,6 +187,12 @@ const char* epikv_strerror(int status);
 /* Validate a configuration without touching the device. */
 int epikv_check_cfg(const epikv_cfg* cfg);
 
+/* sizeof(epikv_cfg) as the library was compiled.  The struct has grown at its
+ * end (kv_format): a program compiled against a header without that has to be
+ * compiled anew, or the library reads and writes past its struct.  One that
+ * loads the library at run time compares this with its own sizeof first. */
+size_t epikv_cfg_bytes(void);
+
 /* Bytes of one token's K or V row in the pool (the slot stride inside a
  * page); 0 for an invalid cfg. */
 size_t epikv_kv_row_bytes(const epikv_cfg* cfg);

@@ -700,6 +700,8 @@ EPIKV_EXPORT const char* epikv_strerror(int status) {
 
 EPIKV_EXPORT int epikv_check_cfg(const epikv_cfg* cfg) { return check_cfg(cfg); }
 
+EPIKV_EXPORT size_t epikv_cfg_bytes(void) { return sizeof(epikv_cfg); }
+
 EPIKV_EXPORT size_t epikv_kv_row_bytes(const epikv_cfg* cfg) {
   return check_cfg(cfg) ? 0 : (size_t)row_bytes(cfg);
 }

@@ -58,7 +58,7 @@ EXPORTED = ("epikv_default_cfg", "epikv_strerror", "epikv_check_cfg",
             "epikv_kv_row_bytes", "epikv_default_rope", "epikv_check_rope",
             "epikv_rope_table_bytes", "epikv_rope_table", "epikv_rope",
             "epikv_append", "epikv_read", "epikv_attend_workspace_bytes",
-            "epikv_attend")
+            "epikv_attend", "epikv_cfg_bytes")
 
 
 class EpikvError(RuntimeError):
@@ -152,6 +152,12 @@ class AttendIO(ctypes.Structure):
 _lib = None
 
 
+def _same_cfg(nbytes):
+    if nbytes != ctypes.sizeof(Cfg):
+        raise RuntimeError(f"{LIB_PATH}: its epikv_cfg has {nbytes} bytes, this binding's {ctypes.sizeof(Cfg)}: "
+                           "build the library anew")
+
+
 def lib() -> ctypes.CDLL:
     """Load libepikv.so (raises if it has not been built)."""
     global _lib
@@ -203,6 +209,7 @@ def lib() -> ctypes.CDLL:
         "epikv_evict_step": (ctypes.c_int, [cfgp, ctypes.POINTER(StepIO), P]),
         "epikv_evict_step_noalloc": (ctypes.c_int,
                                      [cfgp, ctypes.POINTER(StepIO), P]),
+        "epikv_cfg_bytes": (sz, []),
         "epikv_kv_row_bytes": (sz, [cfgp]),
         "epikv_default_rope": (ctypes.c_int, [ropep]),
         "epikv_check_rope": (ctypes.c_int, [ropep]),
@@ -219,6 +226,7 @@ def lib() -> ctypes.CDLL:
         fn = getattr(L, name)
         fn.restype = res
         fn.argtypes = args
+    _same_cfg(L.epikv_cfg_bytes())
     _lib = L
     return L
 
