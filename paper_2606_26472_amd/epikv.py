@@ -633,16 +633,20 @@ def epikv_rope(rope: Rope, table, dtype, batch, chunk, n_heads, head_dim, x,
                   and table.is_contiguous() and positions.is_contiguous())
     except AttributeError:  # (addresses)
         enough = False
-    if not enough:
+    if enough:
+        table, positions = table.data_ptr(), positions.data_ptr()
+    else:
         _expect_table(rope, table)
         _expect_rows(positions, batch, ld_pos or 1, "positions")
+        table, positions = _ptr(table), _ptr(positions)
     if seq_status is not None:
         _expect_rows(seq_status, batch, 1, "seq_status")
-    _check(lib().epikv_rope(
-        ctypes.byref(rope), _ptr(table), int(dtype), int(batch), int(chunk),
-        int(n_heads), int(head_dim), ctypes.byref(xr), ctypes.byref(yr),
-        _ptr(positions), int(ld_pos), int(transpose), _ptr(seq_status),
-        _stream(stream)), "epikv_rope")
+        seq_status = _ptr(seq_status)
+    status = (_lib or lib()).epikv_rope(
+        rope, table, int(dtype), int(batch), int(chunk), int(n_heads), int(head_dim), xr, yr, positions,
+        int(ld_pos), int(transpose), seq_status, _stream(stream))
+    if status != EPIKV_OK:
+        _check(status, "epikv_rope")
 
 
 def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
