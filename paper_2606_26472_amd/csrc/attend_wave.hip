@@ -13,8 +13,6 @@
 // Bound by HBM: 32 sequences of 8k-32k tokens (8 KV heads of 128, 4 query heads
 // each) 2.69 GB in 406 us, 6.6 TB/s; in 4 bits 0.72 GB in 138 us, 5.2 TB/s, with
 // the vector units busy 45 % of the time.  One sequence of 4k: 8 us, latency.
-#include <type_traits>
-
 #include "attend_impl.h"
 
 namespace epikv {
@@ -577,32 +575,27 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
   } else {
     if (!find_share<kSplitBatch / 64>(g, p.n_teams, (int)team, lane, x)) return;
   }
-  auto walk = [&](auto once) {
-    for (;;) {
-      const int u = units_of(x.t);
-      if (u > 0) {
-        const int u0 = x.lo - x.before, u1 = min(u, x.hi - x.before);
-        // (who has a sequence's first unit tells the join where its shares are)
-        if (p.split && u0 == 0 && h == 0 && lane == 0)
-          p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
-        attend_share<D, Q4, decltype(once)::value>(a, p, x.b, h, x.t, u0, u1, u0 == 0 && u1 == u,
-                                                   (int)team + x.b, s_lds[wave], lane);
-        x.lo = x.before + u1;
-        x.before += u;
-      }
-      if (x.lo >= x.hi) break;
-      x.t = seq_tokens(g, ++x.b);
+  // (without shares a team knows one sequence of more than a thousand: too many
+  // to be there at the next token, unless all are short)
+  const bool once = LARGE && (!p.split || (int64_t)x.total * (2 * kUnit) * g.row_bytes > kCacheBytes);
+  for (;;) {
+    const int u = units_of(x.t);
+    if (u > 0) {
+      const int u0 = x.lo - x.before, u1 = min(u, x.hi - x.before);
+      // (who has a sequence's first unit tells the join where its shares are)
+      if (p.split && u0 == 0 && h == 0 && lane == 0)
+        p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
+      const bool whole = u0 == 0 && u1 == u;
+      if (once)
+        attend_share<D, Q4, LARGE>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, s_lds[wave], lane);
+      else
+        attend_share<D, Q4, false>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, s_lds[wave], lane);
+      x.lo = x.before + u1;
+      x.before += u;
     }
-  };
-  if constexpr (LARGE) {
-    // (without shares a team knows one sequence of more than a thousand: too
-    // many to be there at the next token, unless all are short)
-    if (!p.split || (int64_t)x.total * (2 * kUnit) * g.row_bytes > kCacheBytes) {
-      walk(std::true_type{});
-      return;
-    }
+    if (x.lo >= x.hi) break;
+    x.t = seq_tokens(g, ++x.b);
   }
-  walk(std::false_type{});
 }
 
 // Joins the shares of one row: a workgroup per (sequence, query row), its
