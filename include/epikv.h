@@ -117,7 +117,8 @@ typedef enum epikv_compact_mode {
  * codes (two to a byte, the lower channel in the low half), then
  * n_kv_heads*head_dim/32 scale bytes, heads outermost in both, padded to a
  * multiple of 16 bytes and to 128 at least (the padding is never written):
- * 4.25 bits a value.
+ * 4.25 bits a value and what the padding adds (8 heads of 128: nothing; 4 of 64:
+ * 4.5 in all; one of 64: 16, as in bf16).
  */
 typedef enum epikv_kv_format {
   EPIKV_KV_BF16 = 0,

@@ -5,7 +5,7 @@
 // maximum `top` grows.  Up to 16 query rows per KV head (tokens times heads of
 // its group) are bound by reading the rows and go to a wavefront per share of
 // a sequence (attend_wave.hip); more are bound by the matrix cores and go to
-// workgroups of 128 rows (attend_tile.hip).
+// workgroups of 256 rows, or of 128 (attend_tile.hip).
 #include "attend_impl.h"
 
 namespace epikv {

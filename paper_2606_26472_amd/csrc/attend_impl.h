@@ -17,7 +17,7 @@ constexpr int kUnit = 32;
 
 // One sequence's units are cut over several teams of wavefronts when the
 // batch is small: all sequences' units in a row, cut into even shares (of one
-// unit at least: 4224 slots 16.5 us in shares of two, 15.3 of one), so that
+// unit at least: 4224 slots 14.2 us in shares of two, 13.1 of one), so that
 // ragged lengths cost no balance.  A team's share may
 // span sequences; its part of sequence b goes to partial slot team + b, which
 // no other (team, sequence) pair of the staircase has.
@@ -75,7 +75,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 
 // Query rows per KV head up to which the wavefront kernel is taken: the columns
 // of one of its instructions.  (At 32 rows of 128 channels over 8 x 8192 slots
-// it takes 103 us with two sets of them, the tile kernel 71; at 16 rows 67.)
+// it took 103 us with two sets of them, the tile kernel takes 60; 16 rows 62.)
 constexpr int kWaveRows = 16;
 size_t attend_wave_workspace(int B, int H, int R, int d);
 hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s);

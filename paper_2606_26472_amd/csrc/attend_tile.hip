@@ -12,8 +12,8 @@
 //
 // Bound by the matrix cores and the softmax's arithmetic together (32 scores
 // a lane and tile: 32 exponentials beside 32 matrix instructions).  A chunk of
-// 4096 tokens over 16k slots (32 query heads of 128) 905 us, 1.06 PFLOP/s; 8
-// chunks of 128 over 32k in 4 bits 560 us, 0.98.
+// 4096 tokens over 16k slots (32 query heads of 128) 890-930 us by box, 1.03-1.08
+// PFLOP/s; 8 chunks of 128 over 32k in 4 bits 560-580 us, 0.94-0.98.
 #include <type_traits>
 
 #include "attend_impl.h"
@@ -478,6 +478,10 @@ __global__ __launch_bounds__(256) void k_attend_tile_join(AttendArgs a, TilePlan
         some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
 }
 
+// Pieces of a row tile at most.  How long the sequences are only the device
+// knows: 8, 16, 32 pieces take 228, 126, 81 us for 17 tokens over 64k slots (8 KV
+// heads), 58.0, 57.5, 56.0 for 200 over 8k, but 23.3, 20.0, 21.1 for 17 over 4000
+// and 13.7, 13.9, 15.8 for 40 over 1000.
 constexpr int kMaxSplits = 16;
 
 // Wavefronts of a workgroup: eight halve what each of them does to bring a tile
@@ -499,7 +503,8 @@ TilePlan tile_plan(int B, int H, int R, int d) {
   const int64_t blocks = (int64_t)B * H * p.row_tiles;
   const int64_t want = cus * 8 / p.waves;
   p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, want / blocks));
-  // (rows of 256 channels have one workgroup to a unit, the next when it ends)
+  // (rows of 256 channels have one workgroup to a unit, the next when it ends;
+  // two sequences in pairs 45.0 us, as without, for 1000 tokens of 4 KV heads)
   p.paired = p.waves == 4 && d <= 128 && p.splits == 1 && B == 1 && blocks <= want;
   p.part_o = nullptr;
   p.part_ml = nullptr;

@@ -491,8 +491,8 @@ struct Share {
 // Units of a share: enough to leave no team without, and, where the teams
 // would outnumber what is worth joining, enough to balance a step's time with
 // a join's per share (about 40 to 1, so sqrt(units of a sequence / 40)).  One KV
-// head, 64k slots: 46 us in single units, 18 so; 600k: 90, 75; one sequence of
-// 4k slots, 8 KV heads, 13.3 both.
+// head, 64k slots: 51 us in single units, 19 so; 600k: 92, 76; one sequence of
+// 4k slots, 8 KV heads, 13.1 both.
 __device__ __forceinline__ int units_per_team(int total, int n_teams, int B) {
   const int balanced = (int)sqrtf((float)total / (40.f * (float)B));
   return max(max(1, balanced), (total + n_teams - 1) / n_teams);
@@ -569,8 +569,8 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
       return;
     }
   } else if (g.B <= 64) {
-    // (a launch fetches its instructions anew: one sequence of 4k slots 15.2 us
-    // with this, 16.3 through the code for 1024)
+    // (a launch fetches its instructions anew: one sequence of 4k slots 13.1 us
+    // with this, 15.1 through the code for 1024)
     if (!find_share<1>(g, p.n_teams, (int)team, lane, x)) return;
   } else {
     if (!find_share<kSplitBatch / 64>(g, p.n_teams, (int)team, lane, x)) return;
