@@ -12,7 +12,7 @@
 //
 // Bound by the matrix cores and the softmax's arithmetic together (32 scores
 // a lane and tile: 32 exponentials beside 32 matrix instructions).  A chunk of
-// 4096 tokens over 16k slots (32 query heads of 128) 890-930 us by box, 1.03-1.08
+// 4096 tokens over 16k slots (32 query heads of 128) 890-930 us by machine, 1.03-1.08
 // PFLOP/s; 8 chunks of 128 over 32k in 4 bits 560-580 us, 0.94-0.98.
 #include <type_traits>
 
