@@ -27,6 +27,9 @@
  * and values into the pages, rotated on the way), epikv_attend (attention
  * over the pages) and epikv_read (rows back as bf16).  The pages hold bf16
  * rows or rows of 4 bits (epikv_kv_format); the step moves either.
+ * epikv_attend_weigh also sums the attention's weights per slot, for steps
+ * that evict by them; epikv_rope_axes and epikv_append_axes take positions on
+ * several axes.
  *
  * Conventions shared by every entry point
  * ---------------------------------------
@@ -670,6 +673,55 @@ int epikv_rope(const epikv_rope_cfg* rope, const float* table, int32_t dtype,
                const int32_t* positions, int64_t ld_pos, int32_t transpose,
                int32_t* seq_status, hipStream_t stream);
 
+#define EPIKV_MAX_AXES 4
+
+/* Which pairs an axis turns. */
+typedef enum epikv_axes_order {
+  EPIKV_AXES_SECTIONS = 0,  /* the first pairs[0] pairs by axis 0, the next pairs[1] by axis 1, ... */
+  EPIKV_AXES_TURNS = 1      /* the axes take turns, 0, 1, ... and again from 0; one whose
+                               pairs are used up drops out */
+} epikv_axes_order;
+
+/* The frequencies of an axis' pairs. */
+typedef enum epikv_axes_frequencies {
+  EPIKV_AXES_SHARED = 0,  /* pair i of the head has f_i, whichever axis turns it */
+  EPIKV_AXES_APART = 1    /* the k-th pair of axis a has f_k of a rotation of 2*pairs[a]
+                             channels (r = 2*pairs[a] in epikv_rope_scaling) */
+} epikv_axes_frequencies;
+
+/* Positions on several axes, as of time, height and width (host struct): a
+ * token has one for each, and every pair is turned by its axis' position. */
+typedef struct epikv_axes {
+  int32_t n_axes;                  /* 1..EPIKV_MAX_AXES */
+  int32_t pairs[EPIKV_MAX_AXES];   /* of each axis, >= 1; rotary_dim / 2 together */
+  int32_t order;                   /* epikv_axes_order */
+  int32_t frequencies;             /* epikv_axes_frequencies */
+} epikv_axes;
+
+/* Validate both without touching the device. */
+int epikv_check_axes(const epikv_rope_cfg* rope, const epikv_axes* axes);
+
+/* epikv_rope_table for positions on several axes, of epikv_rope_table_bytes
+ * too: [n_pos][r / 2][2], at each position what every pair has whose axis is
+ * there (for SHARED frequencies the same table; for APART ones NTK needs
+ * pairs[a] >= 2). */
+int epikv_rope_axes_table(const epikv_rope_cfg* rope, const epikv_axes* axes, float* table, hipStream_t stream);
+
+/*
+ * epikv_rope_axes -- epikv_rope with a position on every axis.
+ *
+ * positions: int32, ld_pos = 0: [batch][n_axes], those of the sequence's first
+ * token, the rest follow one by one on every axis (as text does); else
+ * [batch][n_axes][ld_pos >= chunk].  A token with one of its positions out of
+ * range is not written (and flagged).  With equal positions on all axes and
+ * SHARED frequencies the result is epikv_rope's, bit for bit.
+ * Other arguments, transpose among them, as there.
+ */
+int epikv_rope_axes(const epikv_rope_cfg* rope, const epikv_axes* axes, const float* table, int32_t dtype,
+                    int32_t batch, int32_t chunk, int32_t n_heads, int32_t head_dim, const epikv_rows* x,
+                    const epikv_rows* y, const int32_t* positions, int64_t ld_pos, int32_t transpose,
+                    int32_t* seq_status, hipStream_t stream);
+
 /* Arguments of epikv_append (host struct; device pointers unless marked). */
 typedef struct epikv_append_io {
   int32_t chunk;
@@ -712,6 +764,17 @@ typedef struct epikv_append_io {
  * Pages of different sequences may be shared only where neither appends.
  */
 int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io, hipStream_t stream);
+
+/*
+ * epikv_append_axes -- epikv_append with keys and queries turned by positions
+ * on several axes.  io->rope must be given; io->positions and io->ld_pos are
+ * as for epikv_rope_axes.  Several tokens of an image may share a position, so
+ * the ids written to io->pos are an input of their own (needed with io->pos):
+ * int32, ld_ids = 0: [batch], the id of the sequence's first new token, the
+ * rest follow; else [batch][ld_ids >= chunk].
+ */
+int epikv_append_axes(const epikv_cfg* cfg, const epikv_append_io* io, const epikv_axes* axes, const int32_t* ids,
+                      int64_t ld_ids, hipStream_t stream);
 
 /* Arguments of epikv_read. */
 typedef struct epikv_read_io {
@@ -775,6 +838,50 @@ size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t
  * share one must not overlap in time.  May be captured in a HIP graph.
  */
 int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io, hipStream_t stream);
+
+/* Where epikv_attend_weigh puts its sums. */
+typedef struct epikv_weigh_io {
+  const float* old;   /* [B][ld_s] sums so far; may be `weights` itself (in
+                         place), NULL: none */
+  float* weights;     /* [B][ld_s] */
+  int64_t ld_s;
+  float keep_old;     /* [0, 1]: how much stays of the sums of the slots before
+                         the new tokens (a forgetting factor), */
+  float keep_new;     /* and of those of the new tokens (0 where this layer is
+                         the first to see them, 1 for the others) */
+  float gain;         /* > 0: of this call's weights */
+  int32_t watch;      /* queries counted: of the sequence's last `watch` new
+                         tokens; 0 = all */
+} epikv_weigh_io;
+
+/* Device scratch of epikv_attend_weigh with page tables of ld_pt entries
+ * (0: none needed, or invalid arguments). */
+size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads, int64_t ld_pt,
+                                          int32_t watch);
+
+/*
+ * epikv_attend_weigh -- epikv_attend, and how much its queries looked at every
+ * slot: the signal of the eviction policies that need the attention's weights
+ * (Sec. 2, Table 1: accumulated attention).  For j < n_cached[b]
+ *   weights[b][j] = keep * old[b][j] + gain * sum over the counted tokens c and
+ *                   all query heads h of exp(scale*(q . k_j) - lse[b][h][c])
+ * with keep = keep_old, or keep_new for the new tokens' slots; a sum kept by 0
+ * is not read, whatever it holds.  A token adds nothing to slots it does not
+ * see, nor where it sees nothing; slots in pages out of range get nothing
+ * added.  Entries from n_cached[b] on are left as they are, and so is a
+ * sequence without new tokens or with counts out of range; a slot >= ld_s has
+ * no place (not written; flags the sequence).  Weights and sums are float32,
+ * added in a fixed order.
+ * The sums are scores of the slots as epikv_select takes them: added up over
+ * the layers, they go to epikv_evict_step (chunk = 0, `scores`), which moves
+ * them with the rows.
+ * weights and old: 4-byte aligned; weights overlaps no other argument but old,
+ * which is weights itself or apart from it (EPIKV_EALIAS).  io as for
+ * epikv_attend, its workspace of epikv_attend_weigh_workspace_bytes(...); out
+ * and lse are those of epikv_attend, bit for bit.
+ */
+int epikv_attend_weigh(const epikv_cfg* cfg, const epikv_attend_io* io, const epikv_weigh_io* weigh,
+                       hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -130,3 +130,55 @@ def attend(q, k, v, n_new, scale, ok=None):
             w /= w.sum()
             out[c, h], mag[c, h] = w @ vv, w @ np.abs(vv)
     return out, lse, mag, size
+
+
+def attend_weights(q, k, n_new, scale, ok=None):
+    """w [n_new][Hq][n]: how much every query looks at every slot (softmax
+    over what it sees), arguments as for attend."""
+    n, H, d = k.shape
+    Hq = q.shape[1]
+    w = np.zeros((n_new, Hq, n))
+    for c in range(n_new):
+        see = np.arange(n) <= n - n_new + c
+        if ok is not None:
+            see &= ok
+        for h in range(Hq):
+            s = np.where(see, scale * (k[:, h * H // Hq] @ q[c, h]), -np.inf)
+            if s.max() != -np.inf:  # (NaN goes on)
+                e = np.where(see, np.exp(s - s.max()), 0.0)
+                w[c, h] = e / e.sum()
+    return w
+
+
+def weigh(w, old, n_new, keep_old, keep_new, gain, watch):
+    """Sums per slot of the weights of the last `watch` (0: all) new tokens,
+    on what is kept of the old ones."""
+    n = w.shape[2]
+    keep = np.where(np.arange(n) < n - n_new, keep_old, keep_new)
+    kept = np.where(keep > 0, keep * old, 0.0) if old is not None else np.zeros(n)
+    first = max(0, n_new - watch) if watch else 0
+    return kept + gain * w[first:].sum((0, 1))
+
+
+def axes_of_pairs(pairs, turns):
+    """Every pair's axis and its place there: whole sections one after the
+    other, or the axes in turns, those used up left out."""
+    if not turns:
+        return ([a for a, n in enumerate(pairs) for _ in range(n)],
+                [i for n in pairs for i in range(n)])
+    axis, place = [], []
+    for i in range(max(pairs)):
+        for a, n in enumerate(pairs):
+            if i < n:
+                axis.append(a)
+                place.append(i)
+    return axis, place
+
+
+def rope_axes_frequencies(pairs, turns, apart, theta, *args, **kw):
+    """Radians a position of every pair: those of one rotation, or each axis'
+    pairs as a rotation of their own."""
+    if not apart:
+        return rope_frequencies(2 * sum(pairs), theta, *args, **kw)
+    own = [rope_frequencies(2 * n, theta, *args, **kw) for n in pairs]
+    return np.array([own[a][i] for a, i in zip(*axes_of_pairs(pairs, turns))])

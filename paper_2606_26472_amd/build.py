@@ -34,8 +34,9 @@ SOURCES = ["epikv_api.hip", "score_hs.hip", "score_lagkv.hip", "zscore.hip",
            "select.hip", "compact.hip", "compact_inplace.hip", "score_tokens.hip",
            "smooth_resolve.hip", "step_prep.hip",
            "score_select.hip", "select_multi.hip", "noalloc.hip",
-           "cache_api.hip", "rope.hip", "append.hip", "attend.hip",
-           "attend_wave.hip", "attend_tile.hip"]
+           "cache_api.hip", "rope.hip", "append.hip", "append_axes.hip",
+           "attend.hip", "attend_wave.hip", "attend_tile.hip",
+           "attend_weigh.hip"]
 
 ARCH = "gfx950"
 CXXFLAGS = [

@@ -32,6 +32,35 @@ int check_rope_cfg(const epikv_rope_cfg* r) {
   return EPIKV_OK;
 }
 
+int check_axes(const epikv_rope_cfg* r, const epikv_axes* x) {
+  const int st = check_rope_cfg(r);
+  if (st) return st;
+  if (!x) return EPIKV_EINVAL_NULL;
+  if (x->order < EPIKV_AXES_SECTIONS || x->order > EPIKV_AXES_TURNS) return EPIKV_EINVAL_PARAM;
+  if (x->frequencies < EPIKV_AXES_SHARED || x->frequencies > EPIKV_AXES_APART) return EPIKV_EINVAL_PARAM;
+  if (x->n_axes < 1 || x->n_axes > EPIKV_MAX_AXES) return EPIKV_EINVAL_SHAPE;
+  const int least = x->frequencies == EPIKV_AXES_APART && r->scaling == EPIKV_ROPE_NTK ? 2 : 1;
+  int64_t sum = 0;
+  for (int a = 0; a < x->n_axes; ++a) {
+    if (x->pairs[a] < least) return EPIKV_EINVAL_SHAPE;
+    sum += x->pairs[a];
+  }
+  return sum == r->rotary_dim / 2 ? EPIKV_OK : EPIKV_EINVAL_SHAPE;
+}
+
+// Every pair's axis and its place there, of checked axes.
+void deal_pairs(const epikv_axes* x, uint8_t (&axis)[512], uint16_t (&place)[512]) {
+  int used[EPIKV_MAX_AXES] = {0, 0, 0, 0};
+  int total = 0, a = 0;
+  for (int k = 0; k < x->n_axes; ++k) total += x->pairs[k];
+  for (int i = 0; i < total; ++i) {
+    while (used[a] == x->pairs[a]) a = (a + 1) % x->n_axes;
+    axis[i] = (uint8_t)a;
+    place[i] = (uint16_t)used[a]++;
+    if (x->order == EPIKV_AXES_TURNS) a = (a + 1) % x->n_axes;
+  }
+}
+
 // Query heads: a multiple of the KV heads, the rows of one KV head counted in
 // 32 bits.
 bool heads_fit(int32_t chunk, int32_t n_kv_heads, int32_t n_heads) {
@@ -156,6 +185,38 @@ RopeArg rope_arg(const epikv_rope_cfg* r, const float* table, const int32_t* pos
   return a;
 }
 
+// Slots that a page table of ld_pt entries covers.
+int32_t slots_of(const epikv_cfg* c, int64_t ld_pt) {
+  return (int32_t)std::min<int64_t>(std::min<int64_t>(ld_pt, INT32_MAX) * c->page_size, kMaxTokens);
+}
+
+RopeAxesArg rope_axes_arg(const epikv_rope_cfg* r, const epikv_axes* x, const float* table,
+                          const int32_t* positions, int64_t ld_pos, int32_t transpose) {
+  RopeAxesArg a = {};
+  static_cast<RopeArg&>(a) = rope_arg(r, table, positions, ld_pos, transpose);
+  a.n_axes = x->n_axes;
+  uint8_t axis[512];
+  uint16_t place[512];
+  deal_pairs(x, axis, place);
+  for (int i = 0; i < r->rotary_dim / 2; ++i) a.axis[i / 8] |= (uint16_t)(axis[i] << (2 * (i % 8)));
+  return a;
+}
+
+RopeTableArgs table_args(const epikv_rope_cfg* rope, float* table) {
+  RopeTableArgs a;
+  a.table = table;
+  a.n_pos = rope->n_pos;
+  a.half = rope->rotary_dim / 2;
+  a.scaling = rope->scaling;
+  a.original = rope->original;
+  a.theta = rope->theta;
+  a.factor = rope->factor;
+  a.low = rope->turns_low;
+  a.high = rope->turns_high;
+  a.amplitude = rope->amplitude;
+  return a;
+}
+
 PagedArgs paged_args(const epikv_cfg* c, const epikv_pool* pool, int32_t layer, int32_t chunk,
                      const int32_t* pt, int64_t ld_pt, const int32_t* n_cached,
                      const int32_t* n_new, int32_t* status) {
@@ -179,8 +240,7 @@ PagedArgs paged_args(const epikv_cfg* c, const epikv_pool* pool, int32_t layer, 
   for (int sh = 0; sh <= 10; ++sh)
     if ((1 << sh) == c->page_size) a.page_shift = sh;
   a.row_bytes = row_bytes(c);
-  a.max_tokens = (int32_t)std::min<int64_t>(std::min<int64_t>(ld_pt, INT32_MAX) * c->page_size,
-                                            kMaxTokens);
+  a.max_tokens = slots_of(c, ld_pt);
   return a;
 }
 
@@ -218,27 +278,38 @@ EPIKV_EXPORT int epikv_rope_table(const epikv_rope_cfg* rope, float* table, hipS
   if (st) return st;
   if (!table) return EPIKV_EINVAL_NULL;
   if (!aligned16(table)) return EPIKV_EALIGN;
-  RopeTableArgs a;
-  a.table = table;
-  a.n_pos = rope->n_pos;
-  a.half = rope->rotary_dim / 2;
-  a.scaling = rope->scaling;
-  a.original = rope->original;
-  a.theta = rope->theta;
-  a.factor = rope->factor;
-  a.low = rope->turns_low;
-  a.high = rope->turns_high;
-  a.amplitude = rope->amplitude;
-  return launched(launch_rope_table(a, stream));
+  return launched(launch_rope_table(table_args(rope, table), stream));
 }
 
-EPIKV_EXPORT int epikv_rope(const epikv_rope_cfg* rope, const float* table, int32_t dtype,
-                            int32_t batch, int32_t chunk, int32_t n_heads, int32_t head_dim,
-                            const epikv_rows* x, const epikv_rows* y, const int32_t* positions,
-                            int64_t ld_pos, int32_t transpose, int32_t* seq_status,
-                            hipStream_t stream) {
-  int st = check_rope_cfg(rope);
+EPIKV_EXPORT int epikv_check_axes(const epikv_rope_cfg* rope, const epikv_axes* axes) {
+  return check_axes(rope, axes);
+}
+
+EPIKV_EXPORT int epikv_rope_axes_table(const epikv_rope_cfg* rope, const epikv_axes* axes, float* table,
+                                       hipStream_t stream) {
+  const int st = check_axes(rope, axes);
   if (st) return st;
+  if (!table) return EPIKV_EINVAL_NULL;
+  if (!aligned16(table)) return EPIKV_EALIGN;
+  if (axes->frequencies == EPIKV_AXES_SHARED)
+    return launched(launch_rope_table(table_args(rope, table), stream));
+  RopeAxesTableArgs a = {};
+  a.t = table_args(rope, table);
+  uint8_t axis[512];
+  deal_pairs(axes, axis, a.place);
+  for (int i = 0; i < a.t.half; ++i) a.count[i] = (uint16_t)axes->pairs[axis[i]];
+  return launched(launch_rope_axes_table(a, stream));
+}
+
+namespace epikv {
+namespace {
+
+// What epikv_rope and epikv_rope_axes check alike (rope is checked), and their
+// arguments but the positions.
+template <class Args>
+int prepare_rope(Args& a, const epikv_rope_cfg* rope, const float* table, int32_t dtype, int32_t batch,
+                 int32_t chunk, int32_t n_heads, int32_t head_dim, const epikv_rows* x, const epikv_rows* y,
+                 const int32_t* positions, int64_t ld_pos, int32_t* seq_status) {
   if (!table || !x || !y) return EPIKV_EINVAL_NULL;
   if (dtype != EPIKV_DTYPE_BF16 && dtype != EPIKV_DTYPE_FP32) return EPIKV_EINVAL_PARAM;
   if (batch < 1 || chunk < 1 || (int64_t)batch * chunk > INT32_MAX) return EPIKV_EINVAL_SHAPE;
@@ -247,7 +318,7 @@ EPIKV_EXPORT int epikv_rope(const epikv_rope_cfg* rope, const float* table, int3
     return EPIKV_EINVAL_SHAPE;
   if (!rope_fits((int64_t)batch * chunk, n_heads, head_dim)) return EPIKV_EINVAL_SHAPE;
   if (!aligned16(table)) return EPIKV_EALIGN;
-  st = check_rows(x);
+  int st = check_rows(x);
   if (st) return st;
   st = check_out_rows(y, batch, chunk, n_heads, head_dim);
   if (st) return st;
@@ -255,21 +326,55 @@ EPIKV_EXPORT int epikv_rope(const epikv_rope_cfg* rope, const float* table, int3
   if (st) return st;
   st = check_alias(x, y, batch, chunk, n_heads, head_dim, dtype == EPIKV_DTYPE_FP32 ? 4 : 2);
   if (st) return st;
-  RopeArgs a;
   a.x = rows_arg(x);
   a.y = rows_arg(y);
-  a.rope = rope_arg(rope, table, positions, ld_pos, transpose);
   a.B = batch;
   a.C = chunk;
   a.heads = n_heads;
   a.d = head_dim;
   a.fp32 = dtype == EPIKV_DTYPE_FP32;
   a.status = seq_status;
+  return EPIKV_OK;
+}
+
+}  // namespace
+}  // namespace epikv
+
+EPIKV_EXPORT int epikv_rope(const epikv_rope_cfg* rope, const float* table, int32_t dtype,
+                            int32_t batch, int32_t chunk, int32_t n_heads, int32_t head_dim,
+                            const epikv_rows* x, const epikv_rows* y, const int32_t* positions,
+                            int64_t ld_pos, int32_t transpose, int32_t* seq_status,
+                            hipStream_t stream) {
+  int st = check_rope_cfg(rope);
+  if (st) return st;
+  RopeArgs a;
+  st = prepare_rope(a, rope, table, dtype, batch, chunk, n_heads, head_dim, x, y, positions, ld_pos, seq_status);
+  if (st) return st;
+  a.rope = rope_arg(rope, table, positions, ld_pos, transpose);
   return launched(launch_rope(a, stream));
 }
 
-EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
-                              hipStream_t stream) {
+EPIKV_EXPORT int epikv_rope_axes(const epikv_rope_cfg* rope, const epikv_axes* axes, const float* table,
+                                 int32_t dtype, int32_t batch, int32_t chunk, int32_t n_heads,
+                                 int32_t head_dim, const epikv_rows* x, const epikv_rows* y,
+                                 const int32_t* positions, int64_t ld_pos, int32_t transpose,
+                                 int32_t* seq_status, hipStream_t stream) {
+  int st = check_axes(rope, axes);
+  if (st) return st;
+  RopeAxesArgs a;
+  st = prepare_rope(a, rope, table, dtype, batch, chunk, n_heads, head_dim, x, y, positions, ld_pos, seq_status);
+  if (st) return st;
+  a.rope = rope_axes_arg(rope, axes, table, positions, ld_pos, transpose);
+  return launched(launch_rope_axes(a, stream));
+}
+
+namespace epikv {
+namespace {
+
+// What epikv_append and epikv_append_axes check alike, and their arguments but
+// the rotation.
+template <class Args>
+int prepare_append(Args& a, const epikv_cfg* cfg, const epikv_append_io* io) {
   if (!cfg || !io) return EPIKV_EINVAL_NULL;
   int st = check_paged(cfg, &io->pool, io->layer, io->chunk, io->page_table, io->ld_pt);
   if (st) return st;
@@ -305,11 +410,9 @@ EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
       return EPIKV_EALIAS;
   }
   if (!append_fits((int64_t)B * C, H, io->q.base ? io->n_heads : 0, d)) return EPIKV_EINVAL_SHAPE;
-  AppendArgs a;
-  memset(&a, 0, sizeof(a));
+  a = {};
   a.pg = paged_args(cfg, &io->pool, io->layer, C, io->page_table, io->ld_pt, io->n_cached,
                     io->n_new, io->seq_status);
-  a.rope = rope_arg(io->rope, io->rope_table, io->positions, io->ld_pos, 0);
   a.k = rows_arg(&io->k);
   a.v = rows_arg(&io->v);
   if (io->q.base) {
@@ -319,7 +422,37 @@ EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
   }
   a.pos = io->pos;
   a.ld_s = io->ld_s;
+  return EPIKV_OK;
+}
+
+}  // namespace
+}  // namespace epikv
+
+EPIKV_EXPORT int epikv_append(const epikv_cfg* cfg, const epikv_append_io* io,
+                              hipStream_t stream) {
+  AppendArgs a;
+  const int st = prepare_append(a, cfg, io);
+  if (st) return st;
+  a.rope = rope_arg(io->rope, io->rope_table, io->positions, io->ld_pos, 0);
   return launched(launch_append(a, is_q4(cfg), stream));
+}
+
+EPIKV_EXPORT int epikv_append_axes(const epikv_cfg* cfg, const epikv_append_io* io, const epikv_axes* axes,
+                                   const int32_t* ids, int64_t ld_ids, hipStream_t stream) {
+  if (!cfg || !io || !axes || !io->rope) return EPIKV_EINVAL_NULL;
+  AppendAxesArgs a;
+  int st = prepare_append(a, cfg, io);
+  if (st) return st;
+  st = check_axes(io->rope, axes);
+  if (st) return st;
+  if (io->pos) {
+    st = check_positions(ids, ld_ids, io->chunk);
+    if (st) return st;
+  }
+  a.rope = rope_axes_arg(io->rope, axes, io->rope_table, io->positions, io->ld_pos, 0);
+  a.rope.ids = ids;
+  a.rope.ld_ids = ld_ids;
+  return launched(launch_append_axes(a, is_q4(cfg), stream));
 }
 
 EPIKV_EXPORT int epikv_read(const epikv_cfg* cfg, const epikv_read_io* io, hipStream_t stream) {
@@ -342,17 +475,24 @@ EPIKV_EXPORT int epikv_read(const epikv_cfg* cfg, const epikv_read_io* io, hipSt
   return launched(launch_read(a, is_q4(cfg), stream));
 }
 
-EPIKV_EXPORT size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t chunk,
-                                                 int32_t n_heads) {
-  if (check_cfg(cfg) || chunk < 1 || chunk > kMaxChunk ||
-      !heads_fit(chunk, cfg->n_kv_heads, n_heads) || (int64_t)cfg->batch * chunk > INT32_MAX)
-    return 0;
-  return attend_workspace(cfg->batch, chunk, cfg->n_kv_heads, n_heads, cfg->head_dim);
+namespace epikv {
+namespace {
+
+bool attend_fits(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads) {
+  return !check_cfg(cfg) && chunk >= 1 && chunk <= kMaxChunk && heads_fit(chunk, cfg->n_kv_heads, n_heads) &&
+         (int64_t)cfg->batch * chunk <= INT32_MAX;
 }
 
-EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
-                              hipStream_t stream) {
-  if (!cfg || !io) return EPIKV_EINVAL_NULL;
+int32_t watched(int32_t watch, int32_t chunk) { return watch ? std::min(watch, chunk) : chunk; }
+
+struct Span {
+  const void* p;
+  size_t n;
+};
+
+// What epikv_attend and epikv_attend_weigh check alike, and the arguments.
+// `spans` receives six arguments that nothing written besides may overlap.
+int prepare_attend(AttendArgs& a, const epikv_cfg* cfg, const epikv_attend_io* io, Span* spans) {
   int st = check_paged(cfg, &io->pool, io->layer, io->chunk, io->page_table, io->ld_pt);
   if (st) return st;
   if (!io->n_cached) return EPIKV_EINVAL_NULL;
@@ -364,21 +504,12 @@ EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
   st = check_out_rows(&io->out, B, C, io->n_heads, d);
   if (st) return st;
   if (rows_meet(&io->out, io->n_heads, &io->q, io->n_heads, B, C, d, 2)) return EPIKV_EALIAS;
-  const size_t n_out = rows_span(&io->out, B, C, io->n_heads, d, 2);
-  const size_t n_q = rows_span(&io->q, B, C, io->n_heads, d, 2);
-  const size_t need = attend_workspace(B, C, H, io->n_heads, d);
-  if (need) {
-    if (!io->workspace || io->workspace_bytes < need) return EPIKV_EWORKSPACE;
-    if (!aligned16(io->workspace)) return EPIKV_EALIGN;
-    const size_t n_lse = io->lse ? (size_t)B * io->n_heads * C * 4 : 0;
-    if (overlap(io->workspace, need, io->q.base, n_q) ||
-        overlap(io->workspace, need, io->out.base, n_out) ||
-        (io->lse && overlap(io->workspace, need, io->lse, n_lse)) ||
-        overlap(io->workspace, need, io->page_table, 4 * (size_t)B * (size_t)io->ld_pt) ||
-        overlap(io->workspace, need, io->n_cached, 4 * (size_t)B))
-      return EPIKV_EALIAS;
-  }
-  AttendArgs a;
+  spans[0] = {io->q.base, rows_span(&io->q, B, C, io->n_heads, d, 2)};
+  spans[1] = {io->out.base, rows_span(&io->out, B, C, io->n_heads, d, 2)};
+  spans[2] = {io->lse, io->lse ? (size_t)B * io->n_heads * C * 4 : 0};
+  spans[3] = {io->page_table, 4 * (size_t)B * (size_t)io->ld_pt};
+  spans[4] = {io->n_cached, 4 * (size_t)B};
+  spans[5] = {io->n_new, io->n_new ? 4 * (size_t)B : 0};
   memset(&a, 0, sizeof(a));
   a.pg = paged_args(cfg, &io->pool, io->layer, C, io->page_table, io->ld_pt, io->n_cached,
                     io->n_new, io->seq_status);
@@ -390,5 +521,89 @@ EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
   a.R = C * a.G;
   const float scale = io->scale > 0.f ? io->scale : 1.f / sqrtf((float)d);
   a.scale2 = scale * 1.4426950408889634f;
+  return EPIKV_OK;
+}
+
+bool meets(const void* p, size_t n, const Span* spans, int n_spans) {
+  for (int i = 0; i < n_spans; ++i)
+    if (spans[i].n && overlap(p, n, spans[i].p, spans[i].n)) return true;
+  return false;
+}
+
+int check_workspace(const epikv_attend_io* io, size_t need, const Span* spans, int n_spans) {
+  if (!need) return EPIKV_OK;
+  if (!io->workspace || io->workspace_bytes < need) return EPIKV_EWORKSPACE;
+  if (!aligned16(io->workspace)) return EPIKV_EALIGN;
+  return meets(io->workspace, need, spans, n_spans) ? EPIKV_EALIAS : EPIKV_OK;
+}
+
+}  // namespace
+}  // namespace epikv
+
+EPIKV_EXPORT size_t epikv_attend_workspace_bytes(const epikv_cfg* cfg, int32_t chunk,
+                                                 int32_t n_heads) {
+  if (!attend_fits(cfg, chunk, n_heads)) return 0;
+  return attend_workspace(cfg->batch, chunk, cfg->n_kv_heads, n_heads, cfg->head_dim);
+}
+
+EPIKV_EXPORT int epikv_attend(const epikv_cfg* cfg, const epikv_attend_io* io,
+                              hipStream_t stream) {
+  if (!cfg || !io) return EPIKV_EINVAL_NULL;
+  AttendArgs a;
+  Span spans[6];
+  int st = prepare_attend(a, cfg, io, spans);
+  if (st) return st;
+  const size_t need = attend_workspace(cfg->batch, io->chunk, cfg->n_kv_heads, io->n_heads, cfg->head_dim);
+  st = check_workspace(io, need, spans, 5);
+  if (st) return st;
   return launched(launch_attend(a, is_q4(cfg), io->workspace, stream));
+}
+
+EPIKV_EXPORT size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads,
+                                                       int64_t ld_pt, int32_t watch) {
+  if (!attend_fits(cfg, chunk, n_heads) || ld_pt < 1 || watch < 0) return 0;
+  return attend_weigh_workspace(cfg->batch, chunk, cfg->n_kv_heads, n_heads, cfg->head_dim,
+                                slots_of(cfg, ld_pt), watched(watch, chunk));
+}
+
+EPIKV_EXPORT int epikv_attend_weigh(const epikv_cfg* cfg, const epikv_attend_io* io,
+                                    const epikv_weigh_io* weigh, hipStream_t stream) {
+  if (!cfg || !io || !weigh) return EPIKV_EINVAL_NULL;
+  AttendArgs a;
+  Span spans[9];
+  int st = prepare_attend(a, cfg, io, spans);
+  if (st) return st;
+  if (!weigh->weights) return EPIKV_EINVAL_NULL;
+  if (weigh->ld_s < 1 || weigh->watch < 0) return EPIKV_EINVAL_SHAPE;
+  if (!(weigh->keep_old >= 0.f && weigh->keep_old <= 1.f) || !(weigh->keep_new >= 0.f && weigh->keep_new <= 1.f) ||
+      !(weigh->gain > 0.f) || !isfinite(weigh->gain))
+    return EPIKV_EINVAL_PARAM;
+  if ((uintptr_t)weigh->weights % 4 || (uintptr_t)weigh->old % 4) return EPIKV_EALIGN;
+  const int B = cfg->batch;
+  const size_t n_sums = 4 * (size_t)B * (size_t)weigh->ld_s;
+  spans[6] = {io->seq_status, io->seq_status ? 4 * (size_t)B : 0};
+  if (meets(weigh->weights, n_sums, spans, 7)) return EPIKV_EALIAS;
+  if (weigh->old && weigh->old != weigh->weights) {
+    if (overlap(weigh->weights, n_sums, weigh->old, n_sums)) return EPIKV_EALIAS;
+    // (what the call writes before it reads them)
+    if (overlap(spans[1].p, spans[1].n, weigh->old, n_sums) ||
+        (spans[2].n && overlap(spans[2].p, spans[2].n, weigh->old, n_sums)))
+      return EPIKV_EALIAS;
+  }
+  spans[7] = {weigh->weights, n_sums};
+  spans[8] = {weigh->old, weigh->old ? n_sums : 0};
+  const int watch = watched(weigh->watch, io->chunk);
+  const size_t need = attend_weigh_workspace(B, io->chunk, cfg->n_kv_heads, io->n_heads, cfg->head_dim,
+                                             a.pg.max_tokens, watch);
+  st = check_workspace(io, need, spans, 9);
+  if (st) return st;
+  WeighArgs w;
+  w.old = weigh->old;
+  w.weights = weigh->weights;
+  w.ld_s = weigh->ld_s;
+  w.keep_old = weigh->old ? weigh->keep_old : 0.f;
+  w.keep_new = weigh->old ? weigh->keep_new : 0.f;
+  w.gain = weigh->gain;
+  w.watch = watch;
+  return launched(launch_attend_weigh(a, w, is_q4(cfg), io->workspace, stream));
 }

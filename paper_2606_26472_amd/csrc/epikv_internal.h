@@ -497,6 +497,14 @@ struct RopeArg {
   int32_t r, n_pos, interleaved, transpose;
 };
 
+// Positions on several axes: [B][n_axes] (ld_pos = 0) or [B][n_axes][ld_pos].
+struct RopeAxesArg : RopeArg {
+  const int32_t* ids;                      // the tokens' ids, as positions of one axis
+  int64_t ld_ids;
+  int32_t n_axes;
+  uint16_t axis[64];                       // two bits a pair, eight pairs a word
+};
+
 // Where the tokens are: the layer's two planes, through the page table.
 struct PagedArgs {
   char* plane[2];                          // K, V
@@ -516,22 +524,34 @@ struct RopeTableArgs {
   double theta, factor, low, high, amplitude;
 };
 
-struct RopeArgs {
+// Every pair's place on its axis and how many pairs that has.
+struct RopeAxesTableArgs {
+  RopeTableArgs t;
+  uint16_t place[512], count[512];
+};
+
+template <class Rope>
+struct RopeArgsOf {
   RowsArg x, y;
-  RopeArg rope;
+  Rope rope;
   int32_t B, C, heads, d;
   int32_t fp32;
   int32_t* status;
 };
+typedef RopeArgsOf<RopeArg> RopeArgs;
+typedef RopeArgsOf<RopeAxesArg> RopeAxesArgs;
 
-struct AppendArgs {
+template <class Rope>
+struct AppendArgsOf {
   PagedArgs pg;
-  RopeArg rope;
+  Rope rope;
   RowsArg k, v, q, q_out;                  // q.base nullptr: none
   int32_t heads;                           // query heads
   int32_t* pos;
   int64_t ld_s;
 };
+typedef AppendArgsOf<RopeArg> AppendArgs;
+typedef AppendArgsOf<RopeAxesArg> AppendAxesArgs;
 
 struct ReadArgs {
   PagedArgs pg;                            // (n_cached: the first slots)
@@ -546,14 +566,29 @@ struct AttendArgs {
   float scale2;                            // scale * log2(e)
 };
 
+// The sums of the attention's weights per slot.
+struct WeighArgs {
+  const float* old;                        // or nullptr
+  float* weights;
+  int64_t ld_s;
+  float keep_old, keep_new, gain;
+  int32_t watch;                           // tokens counted, 1..C
+};
+
 hipError_t launch_rope_table(const RopeTableArgs& a, hipStream_t s);
+hipError_t launch_rope_axes_table(const RopeAxesTableArgs& a, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
+hipError_t launch_rope_axes(const RopeAxesArgs& a, hipStream_t s);
 bool rope_fits(int64_t tokens, int heads, int d);  // one launch reaches it all
 bool append_fits(int64_t tokens, int H, int heads, int d);
 hipError_t launch_append(const AppendArgs& a, bool q4, hipStream_t s);
+hipError_t launch_append_axes(const AppendAxesArgs& a, bool q4, hipStream_t s);
 hipError_t launch_read(const ReadArgs& a, bool q4, hipStream_t s);
 size_t attend_workspace(int B, int C, int H, int heads, int d);
 hipError_t launch_attend(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
+// slots: what the page tables cover (PagedArgs::max_tokens).
+size_t attend_weigh_workspace(int B, int C, int H, int heads, int d, int slots, int watch);
+hipError_t launch_attend_weigh(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 
 // Shared host checks (epikv_api.hip).
 bool aligned16(const void* p);

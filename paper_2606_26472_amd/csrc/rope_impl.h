@@ -43,6 +43,62 @@ __device__ __forceinline__ f32x2 pair_of(const f32x4* cs, int i) {
   return f32x2{cs[i / 2][2 * (i % 2)], cs[i / 2][2 * (i % 2) + 1]};
 }
 
+// Where a token's cosines and sines are: the table's row of its position.
+struct TableRow {
+  int64_t p;
+  // false: the position is out of range
+  __device__ __forceinline__ bool find(const RopeArg& r, int b, int c) {
+    p = position_of(r, b, c);
+    return p >= 0 && p < r.n_pos;
+  }
+  // M pairs from pair i on (a multiple of M, M of 2).
+  template <int M>
+  __device__ __forceinline__ void load(const RopeArg& r, int i, f32x4* cs) const {
+    const f32x4* t = reinterpret_cast<const f32x4*>(r.table + p * (r.r / 2) + i);
+#pragma unroll
+    for (int k = 0; k < M / 2; ++k) cs[k] = t[k];
+  }
+};
+
+// Positions on several axes: every pair is in the row of its axis' position.
+// The rows are read pair by pair, 8 bytes a lane where one position reads 16.
+struct TableRows {
+  uint32_t p[EPIKV_MAX_AXES];
+  __device__ __forceinline__ bool find(const RopeAxesArg& r, int b, int c) {
+    bool in = true;
+#pragma unroll
+    for (int a = 0; a < EPIKV_MAX_AXES; ++a) {
+      // (no branch between the loads; an axis past the last stands for it)
+      const int64_t row = (int64_t)b * r.n_axes + min(a, r.n_axes - 1);
+      const int64_t at = r.ld_pos ? (int64_t)r.positions[row * r.ld_pos + c] : (int64_t)r.positions[row] + c;
+      in &= at >= 0 && at < r.n_pos;
+      p[a] = (uint32_t)at;
+    }
+    return in;
+  }
+  template <int M>
+  __device__ __forceinline__ void load(const RopeAxesArg& r, int i, f32x4* cs) const {
+    const uint32_t axes = (uint32_t)r.axis[i >> 3] >> (2 * (i & 7));
+    const uint32_t row = (uint32_t)r.r / 2;
+#pragma unroll
+    for (int k = 0; k < M; ++k) {
+      const uint32_t lo = axes >> (2 * k) & 1u ? p[1] : p[0], hi = axes >> (2 * k) & 1u ? p[3] : p[2];
+      const float2 t = r.table[(uint64_t)(axes >> (2 * k) & 2u ? hi : lo) * row + (uint32_t)(i + k)];
+      cs[k / 2][2 * (k % 2)] = t.x;
+      cs[k / 2][2 * (k % 2) + 1] = t.y;
+    }
+  }
+};
+
+__device__ __forceinline__ TableRow turns_of(const RopeArg&) { return TableRow{}; }
+__device__ __forceinline__ TableRows turns_of(const RopeAxesArg&) { return TableRows{}; }
+
+// The id of a new token: its position, or where it has several, an input.
+__device__ __forceinline__ int32_t id_of(const RopeArg&, const TableRow& t, int, int) { return (int32_t)t.p; }
+__device__ __forceinline__ int32_t id_of(const RopeAxesArg& r, const TableRows&, int b, int c) {
+  return r.ld_ids ? r.ids[(int64_t)b * r.ld_ids + c] : r.ids[b] + c;
+}
+
 // A 16-byte vector's channels: 8 of bf16, 4 of float32.
 template <bool FP32>
 struct Vec {
@@ -73,8 +129,8 @@ struct Vec {
 // one layout, and in either neighbouring lanes read and write neighbouring
 // vectors, whole lines at a time (32 bytes a lane, past the caches, wrote
 // float32 at a third of the speed).
-template <bool FP32, int U>
-__device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, const RopeArg& r,
+template <bool FP32, int U, class Rope>
+__device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, const Rope& r,
                                            int32_t* status, int b, int c, int h, int step, int it,
                                            int d) {
   using V = Vec<FP32>;
@@ -91,25 +147,16 @@ __device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, c
     ru[i] = ld_stream(xp + (i * step * x.ld_head + lo) * ES);
     rv[i] = ld_stream(xp + (i * step * x.ld_head + hi) * ES);
   }
-  int64_t p = 0;
-  if (r.table) {
-    p = position_of(r, b, c);
-    if (p < 0 || p >= r.n_pos) {
-      raise_flag(status, b);
-      return;
-    }
+  auto turns = turns_of(r);
+  if (r.table && !turns.find(r, b, c)) {
+    raise_flag(status, b);
+    return;
   }
   f32x4 cs[N / 2];
   if (rot) {
     // (N pairs together, or half of them for each vector)
-    const float2* row = r.table + p * (r.r / 2);
-    const f32x4* t = reinterpret_cast<const f32x4*>(row + (r.interleaved ? lo / 2 : lo));
-    const f32x4* t2 = r.interleaved ? reinterpret_cast<const f32x4*>(row + hi / 2) : t + N / 4;
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-      cs[i] = t[i];
-      cs[N / 4 + i] = t2[i];
-    }
+    turns.template load<N / 2>(r, r.interleaved ? lo / 2 : lo, cs);
+    turns.template load<N / 2>(r, r.interleaved ? hi / 2 : lo + N / 2, cs + N / 4);
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {

@@ -45,6 +45,9 @@ MAX_BAND = 32
 KV_BF16, KV_MXFP4 = 0, 1
 DTYPE_BF16, DTYPE_FP32 = 0, 1
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+AXES_SECTIONS, AXES_TURNS = 0, 1
+AXES_SHARED, AXES_APART = 0, 1
+MAX_AXES = 4
 ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4
 
 EXPORTED = ("epikv_default_cfg", "epikv_strerror", "epikv_check_cfg",
@@ -58,7 +61,9 @@ EXPORTED = ("epikv_default_cfg", "epikv_strerror", "epikv_check_cfg",
             "epikv_kv_row_bytes", "epikv_default_rope", "epikv_check_rope",
             "epikv_rope_table_bytes", "epikv_rope_table", "epikv_rope",
             "epikv_append", "epikv_read", "epikv_attend_workspace_bytes",
-            "epikv_attend", "epikv_cfg_bytes")
+            "epikv_attend", "epikv_cfg_bytes", "epikv_check_axes",
+            "epikv_rope_axes_table", "epikv_rope_axes", "epikv_append_axes",
+            "epikv_attend_weigh_workspace_bytes", "epikv_attend_weigh")
 
 
 class EpikvError(RuntimeError):
@@ -118,6 +123,12 @@ class Rope(ctypes.Structure):
                 ("turns_high", ctypes.c_float), ("amplitude", ctypes.c_float)]
 
 
+class Axes(ctypes.Structure):
+    _fields_ = [("n_axes", ctypes.c_int32),
+                ("pairs", ctypes.c_int32 * MAX_AXES),
+                ("order", ctypes.c_int32), ("frequencies", ctypes.c_int32)]
+
+
 class AppendIO(ctypes.Structure):
     _fields_ = [("chunk", ctypes.c_int32), ("layer", ctypes.c_int32),
                 ("pool", Pool), ("page_table", ctypes.c_void_p),
@@ -147,6 +158,13 @@ class AttendIO(ctypes.Structure):
                 ("scale", ctypes.c_float), ("seq_status", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p),
                 ("workspace_bytes", ctypes.c_size_t)]
+
+
+class WeighIO(ctypes.Structure):
+    _fields_ = [("old", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+                ("ld_s", ctypes.c_int64), ("keep_old", ctypes.c_float),
+                ("keep_new", ctypes.c_float), ("gain", ctypes.c_float),
+                ("watch", ctypes.c_int32)]
 
 
 _lib = None
@@ -182,6 +200,7 @@ def lib() -> ctypes.CDLL:
     cfgp = ctypes.POINTER(Cfg)
     poolp = ctypes.POINTER(Pool)
     ropep, rowsp = ctypes.POINTER(Rope), ctypes.POINTER(Rows)
+    axesp = ctypes.POINTER(Axes)
     sig = {
         "epikv_default_cfg": (ctypes.c_int, [cfgp]),
         "epikv_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -221,6 +240,16 @@ def lib() -> ctypes.CDLL:
         "epikv_read": (ctypes.c_int, [cfgp, ctypes.POINTER(ReadIO), P]),
         "epikv_attend_workspace_bytes": (sz, [cfgp, i32, i32]),
         "epikv_attend": (ctypes.c_int, [cfgp, ctypes.POINTER(AttendIO), P]),
+        "epikv_check_axes": (ctypes.c_int, [ropep, axesp]),
+        "epikv_rope_axes_table": (ctypes.c_int, [ropep, axesp, P, P]),
+        "epikv_rope_axes": (ctypes.c_int, [ropep, axesp, P, i32, i32, i32, i32,
+                                           i32, rowsp, rowsp, P, i64, i32, P,
+                                           P]),
+        "epikv_append_axes": (ctypes.c_int, [cfgp, ctypes.POINTER(AppendIO),
+                                             axesp, P, i64, P]),
+        "epikv_attend_weigh_workspace_bytes": (sz, [cfgp, i32, i32, i64, i32]),
+        "epikv_attend_weigh": (ctypes.c_int, [cfgp, ctypes.POINTER(AttendIO),
+                                              ctypes.POINTER(WeighIO), P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -321,6 +350,24 @@ def kv_row_bytes(cfg: Cfg) -> int:
 def attend_workspace_bytes(cfg: Cfg, chunk: int, n_heads: int) -> int:
     return int(lib().epikv_attend_workspace_bytes(ctypes.byref(cfg), int(chunk),
                                                   int(n_heads)))
+
+
+def attend_weigh_workspace_bytes(cfg: Cfg, chunk: int, n_heads: int,
+                                 ld_pt: int, watch: int = 0) -> int:
+    return int(lib().epikv_attend_weigh_workspace_bytes(
+        ctypes.byref(cfg), int(chunk), int(n_heads), int(ld_pt), int(watch)))
+
+
+def axes_of(pairs, order=AXES_SECTIONS, frequencies=AXES_SHARED) -> Axes:
+    """epikv_axes with so many pairs of each axis."""
+    pairs = [int(n) for n in pairs]
+    if len(pairs) > MAX_AXES:
+        raise ValueError(f"{len(pairs)} axes, {MAX_AXES} at most")
+    return Axes(len(pairs), (ctypes.c_int32 * MAX_AXES)(*pairs), int(order), int(frequencies))
+
+
+def check_axes(rope: Rope, axes: Axes) -> int:
+    return lib().epikv_check_axes(ctypes.byref(rope), ctypes.byref(axes))
 
 
 def default_rope(**overrides) -> Rope:
@@ -649,12 +696,58 @@ def epikv_rope(rope: Rope, table, dtype, batch, chunk, n_heads, head_dim, x,
         _check(status, "epikv_rope")
 
 
+def epikv_rope_axes_table(rope: Rope, axes: Axes, table, stream=None):
+    if not isinstance(table, int):
+        have = table.numel() * table.element_size()
+        if have < rope_table_bytes(rope):
+            raise ValueError(f"table holds {have} bytes, {rope_table_bytes(rope)} needed")
+    _check(lib().epikv_rope_axes_table(ctypes.byref(rope), ctypes.byref(axes), _ptr(table), _stream(stream)),
+           "epikv_rope_axes_table")
+
+
+def epikv_rope_axes(rope: Rope, axes: Axes, table, dtype, batch, chunk, n_heads,
+                    head_dim, x, y, positions, ld_pos=0, transpose=False,
+                    seq_status=None, stream=None):
+    """epikv_rope with positions [batch][n_axes], or [batch][n_axes][ld_pos]."""
+    # (as short as epikv_rope, for the same reason)
+    per_seq = max(1, axes.n_axes) * (ld_pos or 1)
+    if x.__class__ is Rows and y.__class__ is Rows:
+        xr, yr = x, y
+    else:
+        for t, what in ((x, "x"), (y, "y")):
+            _expect(t, "float32" if dtype == DTYPE_FP32 else "bfloat16",
+                    (batch, chunk, n_heads, head_dim), what)
+        xr, yr = _as_rows(x), _as_rows(y)
+    try:
+        enough = (table.nbytes >= 4 * rope.n_pos * rope.rotary_dim and table.dtype is _float32
+                  and positions.nbytes >= 4 * batch * per_seq and positions.dtype is _int32
+                  and table.is_contiguous() and positions.is_contiguous())
+    except AttributeError:  # (addresses)
+        enough = False
+    if enough:
+        table, positions = table.data_ptr(), positions.data_ptr()
+    else:
+        _expect_table(rope, table)
+        _expect_rows(positions, batch, per_seq, "positions")
+        table, positions = _ptr(table), _ptr(positions)
+    if seq_status is not None:
+        _expect_rows(seq_status, batch, 1, "seq_status")
+        seq_status = _ptr(seq_status)
+    status = (_lib or lib()).epikv_rope_axes(
+        rope, axes, table, int(dtype), int(batch), int(chunk), int(n_heads), int(head_dim), xr, yr, positions,
+        int(ld_pos), int(transpose), seq_status, _stream(stream))
+    if status != EPIKV_OK:
+        _check(status, "epikv_rope_axes")
+
+
 def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
                    n_new=None, rope: Rope | None = None, table=None,
                    positions=None, ld_pos=0, q=None, q_out=None, pos=None,
-                   ld_s=0, seq_status=None) -> AppendIO:
+                   ld_s=0, seq_status=None, axes: Axes | None = None, ids=None,
+                   ld_ids=0) -> AppendIO:
     """Build the epikv_append_io struct; k, v, q and q_out are tensors
-    [B][chunk][heads][head_dim].  The object keeps what it was built from."""
+    [B][chunk][heads][head_dim].  The object keeps what it was built from.
+    With axes (and ids, where pos is given) it is for epikv_append_axes."""
     for t, like, what in ((v, k, "v"), (q_out, q, "q_out")):
         if t is not None:
             _expect(t, "bfloat16", like.shape, what)
@@ -665,10 +758,12 @@ def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
         _expect_table(rope, table)
     io = AppendIO()
     io._dims = _dims_held((k.shape[0], k.shape[2], k.shape[3]), page_table=(page_table, ld_pt),
-                          n_cached=(n_cached, 1), n_new=(n_new, 1), positions=(positions, ld_pos),
-                          pos=(pos, ld_s), seq_status=(seq_status, 1))
+                          n_cached=(n_cached, 1), n_new=(n_new, 1),
+                          positions=(positions, max(1, int(ld_pos)) * (max(1, axes.n_axes) if axes else 1)),
+                          pos=(pos, ld_s), seq_status=(seq_status, 1), ids=(ids, ld_ids))
     io._keepalive = [page_table, n_cached, n_new, k, v, rope, table, positions,
-                     q, q_out, pos, seq_status]
+                     q, q_out, pos, seq_status, axes, ids]
+    io._axes = None if axes is None else (axes, _ptr(ids), int(ld_ids))
     io.chunk, io.layer, io.pool = int(chunk), int(layer), pool
     io.page_table, io.ld_pt = _ptr(page_table), int(ld_pt)
     io.n_cached, io.n_new = _ptr(n_cached), _ptr(n_new)
@@ -684,8 +779,20 @@ def make_append_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, k, v,
 
 def epikv_append(cfg: Cfg, io: AppendIO, stream=None):
     _same_shape(cfg, io, "epikv_append")
+    if io._axes is not None:
+        raise ValueError("epikv_append: built with axes, for epikv_append_axes")
     _check(lib().epikv_append(ctypes.byref(cfg), ctypes.byref(io),
                               _stream(stream)), "epikv_append")
+
+
+def epikv_append_axes(cfg: Cfg, io: AppendIO, stream=None):
+    """io: make_append_io with axes (and ids)."""
+    _same_shape(cfg, io, "epikv_append_axes")
+    if io._axes is None:
+        raise ValueError("epikv_append_axes: built without axes, for epikv_append")
+    axes, ids, ld_ids = io._axes
+    _check(lib().epikv_append_axes(ctypes.byref(cfg), ctypes.byref(io), ctypes.byref(axes), ids, ld_ids,
+                                   _stream(stream)), "epikv_append_axes")
 
 
 def make_read_io(chunk, pool: Pool, layer, page_table, ld_pt, first, k=None,
@@ -735,12 +842,37 @@ def make_attend_io(chunk, pool: Pool, layer, page_table, ld_pt, n_cached, q, out
     return io
 
 
-def epikv_attend(cfg: Cfg, io: AttendIO, stream=None):
+def _same_attend(cfg: Cfg, io: AttendIO, where):
     if io._dims != (cfg.batch, cfg.head_dim):
-        raise ValueError(f"epikv_attend: built for (batch, head_dim) = {io._dims}, "
+        raise ValueError(f"{where}: built for (batch, head_dim) = {io._dims}, "
                          f"cfg has {(cfg.batch, cfg.head_dim)}")
+
+
+def epikv_attend(cfg: Cfg, io: AttendIO, stream=None):
+    _same_attend(cfg, io, "epikv_attend")
     _check(lib().epikv_attend(ctypes.byref(cfg), ctypes.byref(io),
                               _stream(stream)), "epikv_attend")
+
+
+def make_weigh_io(weights, ld_s, old=None, keep_old=1.0, keep_new=0.0, gain=1.0,
+                  watch=0) -> WeighIO:
+    """Build the epikv_weigh_io struct; weights and old are float32
+    [batch][ld_s].  old may be weights itself: the sums go on in place."""
+    io = WeighIO()
+    io._held = min(_rows_held(t, max(1, int(ld_s)), what, True) for t, what in ((weights, "weights"), (old, "old")))
+    io._keepalive = [weights, old]
+    io.old, io.weights, io.ld_s = _ptr(old), _ptr(weights), int(ld_s)
+    io.keep_old, io.keep_new, io.gain = float(keep_old), float(keep_new), float(gain)
+    io.watch = int(watch)
+    return io
+
+
+def epikv_attend_weigh(cfg: Cfg, io: AttendIO, weigh: WeighIO, stream=None):
+    _same_attend(cfg, io, "epikv_attend_weigh")
+    if weigh._held < cfg.batch:
+        raise ValueError(f"epikv_attend_weigh: sums for {weigh._held} sequences, cfg has {cfg.batch}")
+    _check(lib().epikv_attend_weigh(ctypes.byref(cfg), ctypes.byref(io), ctypes.byref(weigh),
+                                    _stream(stream)), "epikv_attend_weigh")
 
 
 # ---------------------------------------------------------------------------
