@@ -871,7 +871,8 @@ size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, i
  * added.  Entries from n_cached[b] on are left as they are, and so is a
  * sequence without new tokens or with counts out of range; a slot >= ld_s has
  * no place (not written; flags the sequence).  Weights and sums are float32,
- * added in a fixed order.
+ * added in a fixed order; of a token whose largest score passes 2^30, where
+ * float32 no longer tells scores apart, nothing may be added.
  * The sums are scores of the slots as epikv_select takes them: added up over
  * the layers, they go to epikv_evict_step (chunk = 0, `scores`), which moves
  * them with the rows.

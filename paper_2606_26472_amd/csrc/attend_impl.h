@@ -28,6 +28,10 @@ struct WavePlan {
   float* part_o;    // [n_teams + B][H][R][d] unnormalised
   float2* part_ml;  // [n_teams + B][H][R] maximum (base 2) and sum
   int2* shares;     // [B] a sequence's first team and how many it has
+  // where the scores are kept (for the sums of the weights alone):
+  float* kept;      // [B][H][watch * G][ld_kept], of the counted rows
+  int64_t ld_kept;  // slots, a multiple of kUnit
+  int32_t watch;    // tokens counted
 };
 constexpr int kSplitBatch = 1024;  // largest batch whose sequences are cut
 
@@ -73,12 +77,36 @@ __device__ __forceinline__ uint32_t halves_hi(uint32_t lo, uint32_t hi) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A log-sum as the weights take it: a row that sees nothing has -infinity (and
+// so has one whose largest score, past 2^30, is less exact than what its
+// exponential can bear); every weight is 0 then.
+__device__ __forceinline__ float lse_of_weights(float lse2) { return lse2 == kNegInf ? -kNegInf : lse2; }
+
+// A row's weight of a slot from its score and its log-sum to the base 2.  One
+// at most: what both were rounded to may leave more where they are large.  NaN
+// stays.
+__device__ __forceinline__ float weight_of(float score, float scale2, float lse2) {
+  const float y = fmaf(score, scale2, -lse2);
+  return exp2_fast(y > 0.f ? 0.f : y);
+}
+
+// A slot's sum: what is kept of the old one and this call's.
+__device__ __forceinline__ void write_sum(const WeighArgs& w, int b, int j, const SeqTokens& t, float sum) {
+  const int64_t at = (int64_t)b * w.ld_s + j;
+  const float keep = j < t.n - t.nn ? w.keep_old : w.keep_new;
+  const float kept = keep != 0.f ? keep * w.old[at] : 0.f;  // (kept by 0: not read)
+  w.weights[at] = fmaf(w.gain, sum, kept);
+}
+
 // Query rows per KV head up to which the wavefront kernel is taken: the columns
 // of one of its instructions.  (At 32 rows of 128 channels over 8 x 8192 slots
 // it took 103 us with two sets of them, the tile kernel takes 60; 16 rows 62.)
 constexpr int kWaveRows = 16;
 size_t attend_wave_workspace(int B, int H, int R, int d);
 hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
+// The same, its scores kept and the weights summed.
+size_t weigh_wave_workspace(int B, int H, int R, int d, int G, int slots, int watch);
+hipError_t launch_weigh_wave(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 size_t attend_tile_workspace(int B, int H, int R, int d);
 hipError_t launch_attend_tile(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 

@@ -50,13 +50,10 @@ __global__ __launch_bounds__(256) void k_weigh(AttendArgs a, WeighArgs w, int sl
           }
         }
         const float lse = a.lse[((int64_t)b * a.heads + hq) * g.C + c];
-        if (lse != kNegInf) sum += exp2_fast(fmaf(s, a.scale2, -lse * 1.4426950408889634f));
+        sum += weight_of(s, a.scale2, lse_of_weights(lse * 1.4426950408889634f));
       }
   }
-  const int64_t at = (int64_t)b * w.ld_s + j;
-  const float keep = j < old ? w.keep_old : w.keep_new;
-  const float kept = keep != 0.f ? keep * w.old[at] : 0.f;
-  w.weights[at] = kept + w.gain * sum;
+  write_sum(w, b, j, t, sum);
 }
 
 size_t lse_bytes(int B, int C, int heads) { return ((size_t)B * C * heads * 4 + 255) / 256 * 256; }
@@ -64,10 +61,13 @@ size_t lse_bytes(int B, int C, int heads) { return ((size_t)B * C * heads * 4 + 
 }  // namespace
 
 size_t attend_weigh_workspace(int B, int C, int H, int heads, int d, int slots, int watch) {
+  const int G = heads / H, R = C * G;
+  if (R <= kWaveRows) return weigh_wave_workspace(B, H, R, d, G, slots, watch);
   return lse_bytes(B, C, heads) + attend_workspace(B, C, H, heads, d);
 }
 
 hipError_t launch_attend_weigh(const AttendArgs& args, const WeighArgs& w, bool q4, void* ws, hipStream_t s) {
+  if (args.R <= kWaveRows) return launch_weigh_wave(args, w, q4, ws, s);
   AttendArgs a = args;
   const PagedArgs& g = a.pg;
   if (!a.lse) a.lse = (float*)ws;
