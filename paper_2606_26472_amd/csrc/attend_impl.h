@@ -29,9 +29,12 @@ struct WavePlan {
   float2* part_ml;  // [n_teams + B][H][R] maximum (base 2) and sum
   int2* shares;     // [B] a sequence's first team and how many it has
   // where the scores are kept (for the sums of the weights alone):
-  float* kept;      // [B][H][watch * G][ld_kept], of the counted rows
-  int64_t ld_kept;  // slots, a multiple of kUnit
+  float* kept;      // [B][H][units][watch * G][kUnit]
+  int32_t units;    // that the page tables cover
   int32_t watch;    // tokens counted
+  __device__ __forceinline__ int64_t kept_at(int b, int h, int unit, int G, int H) const {
+    return (((int64_t)b * H + h) * units + unit) * ((int64_t)watch * G * kUnit);
+  }
 };
 constexpr int kSplitBatch = 1024;  // largest batch whose sequences are cut
 

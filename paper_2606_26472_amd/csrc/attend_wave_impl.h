@@ -190,11 +190,16 @@ constexpr int steps_ahead() {
   return D == 64 ? 2 : 1;
 }
 
+// LDS that a wavefront gathers its scores in: what leaves a compute unit its
+// wavefronts (eight, or four of 256 channels).
+template <int D, bool Q4>
+constexpr int kKeepFloats = ((160 * 1024 / (D == 256 ? 4 : 8) - 1280 - (int)sizeof(Scratch<D, Q4>)) / 4) & ~127;
+
 // Units [u0, u1) of sequence b for KV head h.  whole: the units are all of the
 // sequence's, the result is final; else it goes to partial slot `slot`.
 template <int D, bool Q4, bool ONCE, bool KEEP>
 __device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan& p, int b, int h, const SeqTokens& tk,
-                             int u0, int u1, bool whole, int slot, Scratch<D, Q4>& lds, int lane) {
+                             int u0, int u1, bool whole, int slot, Scratch<D, Q4>& lds, float* keep, int lane) {
   using S = Step<D, Q4>;
   constexpr int KS = S::KS, VC = D / 16;
   const PagedArgs& g = a.pg;
@@ -221,12 +226,18 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan
   const bool real = r < rows;
   const char* qp = a.q.base + (b * a.q.ld_seq + c * a.q.ld_tok + hq * a.q.ld_head) * 2;
   const int lim = real ? tk.n - tk.nn + c + 1 : 0;  // slots it sees
-  // (where the lane's scores go; nullptr: the row is not counted)
-  float* kept = nullptr;
+  // Scores are gathered in LDS and written in runs as long as it holds, past the
+  // caches: memory that reads at its full rate has no room for a few lines of
+  // writes a step.  (32 sequences of 8k-32k tokens, 84 MB of scores beside 2.69 GB
+  // of rows: 587 us for the call with a store a step, 527 in runs through the
+  // caches, 506 past them, 495 with each wavefront's runs in one piece; 431
+  // without the writes.)
+  const int first_kept = KEEP ? max(0, tk.nn - p.watch) * a.G : 0;
+  const int kept_rows = KEEP ? rows - first_kept : 1, in_keep = KEEP ? kKeepFloats<D, Q4> / (kept_rows * kUnit) : 0;
+  float* to_keep = nullptr;  // this lane's place there, if its row is counted
+  int n_kept = 0;            // steps gathered
   if constexpr (KEEP) {
-    const int first = max(0, tk.nn - p.watch) * a.G;
-    if (real && r >= first)
-      kept = p.kept + (((int64_t)b * g.H + h) * (p.watch * a.G) + (r - first)) * p.ld_kept + 4 * q4;
+    if (real && r >= first_kept) to_keep = keep + (r - first_kept) * kUnit + 4 * q4;
   }
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
@@ -329,9 +340,23 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan
       for (int e = 0; e < 8; ++e) x[e] = mine >> ((e < 4 ? 0 : 12) + e) & 1u ? x[e] : kNegInf;
     }
     if constexpr (KEEP) {
-      if (kept) {
-        *reinterpret_cast<f32x4*>(kept + base) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4*>(kept + base + 16) = f32x4{x[4], x[5], x[6], x[7]};
+      if (to_keep) {
+        float* to = to_keep + n_kept * (kept_rows * kUnit);
+        *reinterpret_cast<f32x4*>(to) = f32x4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<f32x4*>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
+      }
+      ++n_kept;
+      if (n_kept == in_keep || base + kUnit >= end) {
+        wave_sync();
+        const int per = kept_rows * (kUnit / 4);  // vectors a step
+        float* out = p.kept + p.kept_at(b, h, base / kUnit + 1 - n_kept, a.G, g.H);
+        for (int i = lane; i < n_kept * per; i += 64) {
+          const int u = i / per;
+          __builtin_nontemporal_store(*reinterpret_cast<const f32x4*>(keep + 4 * i),
+                                      reinterpret_cast<f32x4*>(out + u * (p.watch * a.G * kUnit) + 4 * (i - u * per)));
+        }
+        wave_sync();
+        n_kept = 0;
       }
     }
     float m = x[0];
@@ -568,13 +593,16 @@ constexpr int64_t kCacheBytes = 128 << 20;
 // much, their counts say.
 template <int D, bool Q4, bool LARGE, bool KEEP>
 __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
-  __shared__ __align__(16) Scratch<D, Q4> s_lds[D == 256 ? 4 : 8];
+  // (as many as the workgroup has wavefronts: Scratch, then with KEEP the scores)
+  extern __shared__ __align__(16) char s_dynamic[];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const PagedArgs& g = a.pg;
   const int h = blockIdx.y * p.hw + wave;
   const int64_t team = linear_block();
   if (h >= g.H || team >= p.n_teams) return;
+  Scratch<D, Q4>& lds = reinterpret_cast<Scratch<D, Q4>*>(s_dynamic)[wave];
+  float* keep = reinterpret_cast<float*>(s_dynamic + p.hw * sizeof(Scratch<D, Q4>)) + (KEEP ? wave * kKeepFloats<D, Q4> : 0);
   Share x;
   if (!p.split) {  // a sequence to a team
     x.b = (int)team;
@@ -605,9 +633,9 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
         p.shares[x.b] = make_int2((int)team, (x.before + u - 1) / x.per - (int)team + 1);
       const bool whole = u0 == 0 && u1 == u;
       if (once)
-        attend_share<D, Q4, LARGE, KEEP>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, s_lds[wave], lane);
+        attend_share<D, Q4, LARGE, KEEP>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, lds, keep, lane);
       else
-        attend_share<D, Q4, false, KEEP>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, s_lds[wave], lane);
+        attend_share<D, Q4, false, KEEP>(a, p, x.b, h, x.t, u0, u1, whole, (int)team + x.b, lds, keep, lane);
       x.lo = x.before + u1;
       x.before += u;
     }
@@ -736,7 +764,7 @@ WavePlan wave_plan(int B, int H, int d) {
   p.part_ml = nullptr;
   p.shares = nullptr;
   p.kept = nullptr;
-  p.ld_kept = 0;
+  p.units = 0;
   p.watch = 0;
   return p;
 }
@@ -745,12 +773,16 @@ template <int D, bool KEEP>
 hipError_t launch_shares(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
   const dim3 grid = linear_grid(p.n_teams, p.hw * 64, (a.pg.H + p.hw - 1) / p.hw);
   const dim3 block(p.hw * 64);
+  const auto lds = [&](size_t scratch, int floats) { return (unsigned)(p.hw * (scratch + (KEEP ? floats * 4 : 0))); };
   if (q4)
-    hipLaunchKernelGGL((k_attend_wave<D, true, false, KEEP>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, true, false, KEEP>), grid, block,
+                       lds(sizeof(Scratch<D, true>), kKeepFloats<D, true>), s, a, p);
   else if ((int64_t)a.pg.B * a.pg.max_tokens * 2 * a.pg.row_bytes > kCacheBytes)
-    hipLaunchKernelGGL((k_attend_wave<D, false, true, KEEP>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, false, true, KEEP>), grid, block,
+                       lds(sizeof(Scratch<D, false>), kKeepFloats<D, false>), s, a, p);
   else
-    hipLaunchKernelGGL((k_attend_wave<D, false, false, KEEP>), grid, block, 0, s, a, p);
+    hipLaunchKernelGGL((k_attend_wave<D, false, false, KEEP>), grid, block,
+                       lds(sizeof(Scratch<D, false>), kKeepFloats<D, false>), s, a, p);
   return hipGetLastError();
 }
 

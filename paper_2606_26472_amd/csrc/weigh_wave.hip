@@ -32,7 +32,8 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
   const int2 place = p.split ? p.shares[b] : make_int2(0, 1);
   const int j = j0 + 4 * lane;
   const bool some = j < t.n;  // (scores are there to the end of a unit)
-  const float* kept = p.kept + (int64_t)b * g.H * (p.watch * a.G) * p.ld_kept + j;
+  const float* kept = p.kept + p.kept_at(b, 0, j / kUnit, a.G, g.H) + j % kUnit;
+  const int64_t per_kv_head = p.kept_at(0, 1, 0, a.G, g.H);
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int at = 0; at < rows; at += kWeighRows) {
     const int n = min(kWeighRows, rows - at);
@@ -82,7 +83,7 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
       for (int u = 0; u < AHEAD; ++u) {
         const int q = at + min(i + u * waves, n - 1);
         const int h = q / per_head;
-        x[u] = *reinterpret_cast<const f32x4*>(kept + ((int64_t)h * (p.watch * a.G) + (q - h * per_head)) * p.ld_kept);
+        x[u] = *reinterpret_cast<const f32x4*>(kept + h * per_kv_head + (q - h * per_head) * kUnit);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
@@ -134,7 +135,7 @@ __global__ __launch_bounds__(512) void k_join_weigh(AttendArgs a, WavePlan p, We
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
-int64_t kept_slots(int slots) { return ((int64_t)slots + kUnit - 1) / kUnit * kUnit; }
+int units_in(int slots) { return (slots + kUnit - 1) / kUnit; }
 
 template <int D>
 hipError_t launch_weigh(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, bool q4, hipStream_t s) {
@@ -152,7 +153,7 @@ hipError_t launch_weigh(const AttendArgs& a, const WavePlan& p, const WeighArgs&
 
 size_t weigh_wave_workspace(int B, int H, int R, int d, int G, int slots, int watch) {
   return round256(attend_wave_workspace(B, H, R, d)) + round256((size_t)B * H * R * sizeof(float)) +
-         (size_t)B * H * (watch * G) * kept_slots(slots) * sizeof(float);
+         (size_t)B * units_in(slots) * (H * watch * G) * kUnit * sizeof(float);
 }
 
 hipError_t launch_weigh_wave(const AttendArgs& args, const WeighArgs& w, bool q4, void* ws, hipStream_t s) {
@@ -162,7 +163,7 @@ hipError_t launch_weigh_wave(const AttendArgs& args, const WeighArgs& w, bool q4
   char* at = (char*)ws + round256(attend_wave_workspace(g.B, g.H, a.R, g.d));
   if (!a.lse) a.lse = (float*)at;
   p.kept = (float*)(at + round256((size_t)g.B * g.H * a.R * sizeof(float)));
-  p.ld_kept = kept_slots(g.max_tokens);
+  p.units = units_in(g.max_tokens);
   p.watch = w.watch;
   if (g.d == 64) return launch_weigh<64>(a, p, w, q4, s);
   if (g.d == 128) return launch_weigh<128>(a, p, w, q4, s);
