@@ -36,7 +36,7 @@ SOURCES = ["epikv_api.hip", "score_hs.hip", "score_lagkv.hip", "zscore.hip",
            "score_select.hip", "select_multi.hip", "noalloc.hip",
            "cache_api.hip", "rope.hip", "append.hip", "append_axes.hip",
            "attend.hip", "attend_wave.hip", "attend_tile.hip",
-           "attend_weigh.hip", "weigh_wave.hip"]
+           "attend_weigh.hip", "weigh_wave.hip", "weigh_tile.hip"]
 
 ARCH = "gfx950"
 CXXFLAGS = [

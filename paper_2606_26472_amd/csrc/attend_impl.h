@@ -78,6 +78,19 @@ __device__ __forceinline__ uint32_t halves_hi(uint32_t lo, uint32_t hi) {
   return __builtin_amdgcn_perm(hi, lo, 0x07060302u);
 }
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Rows of D channels in LDS: where the 16-byte chunk c of a row goes (and which
+// chunk a place holds), so that 16 rows' reads of one chunk meet no bank twice.
+template <int D>
+__device__ __forceinline__ int row_chunk(int row, int c) {
+  return c ^ (D == 64 ? (row >> 1) & 7 : row & 15);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A log-sum as the weights take it: a row that sees nothing has -infinity (and
@@ -111,6 +124,9 @@ hipError_t launch_attend_wave(const AttendArgs& a, bool q4, void* ws, hipStream_
 size_t weigh_wave_workspace(int B, int H, int R, int d, int G, int slots, int watch);
 hipError_t launch_weigh_wave(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 size_t attend_tile_workspace(int B, int H, int R, int d);
+size_t weigh_tile_workspace(int B, int H, int G, int d, int slots, int watch);
+// After the attention, whose log-sums are in a.lse.
+hipError_t launch_weigh_tile(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 hipError_t launch_attend_tile(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 
 }  // namespace epikv

@@ -21,15 +21,10 @@
 namespace epikv {
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-}
 
 template <int D>
 struct Tile {
@@ -42,9 +37,7 @@ struct Tile {
   // the writes of decoded rows apart).  The change is an exclusive or of
   // the chunk's number, so a fragment's address is a lane's base address,
   // exclusive or the fragment's offset in the row, plus its rows' offset.
-  __device__ static int key_chunk(int row, int c) {
-    return c ^ (D == 64 ? (row >> 1) & 7 : row & 15);
-  }
+  __device__ static int key_chunk(int row, int c) { return row_chunk<D>(row, c); }
   __device__ static int value_chunk(int row, int c) {
     return c ^ (D == 64 ? (row >> 1) & 1 : row & 3) * 5;
   }
