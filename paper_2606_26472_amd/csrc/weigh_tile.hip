@@ -9,6 +9,8 @@
 // (lane % 32, lane / 32) has query row n's scores of keys 8i + 4g + 0..3, so a
 // row's log-sum is one register a lane, and a key's sum stays in one register
 // a lane from the first row to the last.  Only then do lanes meet.
+#include <type_traits>
+
 #include "attend_impl.h"
 
 namespace epikv {
@@ -32,6 +34,8 @@ struct WeighPlan {
   int32_t slot_tiles, pieces;
   int32_t tokens;        // of a tile of rows: whole tokens where 64 rows hold a token's
   int32_t head_tiles;    // tiles of a token, where they do not
+  uint32_t per_inverse;  // of the rows of a token in a tile: 2^16 / per, rounded up (row / per is exact below 64)
+  int32_t near;          // a tile's queries lie within 2^31 bytes
   int64_t ld;            // of a row of partial sums
   float* part;           // [pieces][B][H][ld]
 };
@@ -39,11 +43,14 @@ struct WeighPlan {
 template <int D, bool Q4>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
   constexpr int NB = key_blocks(D), kKeys = 32 * NB, kSlots = slots_of_group(D);
+  constexpr uint64_t kAllKeys = NB == 2 ? ~0ull : 0xffffffffull;
   constexpr int KS = D / 16;            // instructions of a product
   constexpr int RC = D / 8;             // 16-byte chunks of a row
   constexpr int RPI = 1024 / (D * 2);   // rows a load of a wavefront
   constexpr int NI = kRows / kWaves / RPI;
   __shared__ __align__(1024) char s_q[2][kRows * D * 2];
+  __shared__ float s_neg[2][kRows];  // minus a row's log-sum (minus infinity: no such row)
+  __shared__ int s_lim[2][kRows];    // the slots that it sees
   const PagedArgs& g = a.pg;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -92,53 +99,75 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       }
     }
 
-    // The rows of tile t: tokens from c_of(t), heads of the group from g_of(t).
-    auto c_of = [&](int t) { return c_lo + t / p.head_tiles * p.tokens; };
-    auto g_of = [&](int t) { return t % p.head_tiles * kRows; };
-    const int per = min(a.G, kRows);  // rows of a token in a tile
-    // Row `row` of tile t; false: there is none.
-    auto has_row = [&](int t, int row) {
-      return row / per < min(p.tokens, c_hi - c_of(t)) && g_of(t) + row % per < a.G;
+    // A tile's rows: tokens from c on, heads of the group from g on.
+    struct Rows {
+      int c, g;
     };
-    // (where the lane's rows are from the tile's first one on)
-    int64_t q_off[NI];
+    auto rows_of = [&](int t) {
+      const int c = t / p.head_tiles;
+      return Rows{c_lo + c * p.tokens, (t - c * p.head_tiles) * kRows};
+    };
+    auto after = [&](Rows x) {
+      x.g += kRows;
+      return x.g < a.G ? x : Rows{x.c + p.tokens, 0};
+    };
+    const int per = min(a.G, kRows);  // rows of a token in a tile
+    auto token_of = [&](int row) { return (int)(((uint32_t)row * p.per_inverse) >> 16); };
+    // Whether every row of a tile is there, and whether a row (of token c and head
+    // gr of the tile) is.
+    auto whole = [&](Rows x) {
+      return p.tokens * per == kRows && c_hi - x.c >= p.tokens && a.G - x.g >= per;
+    };
+    auto has_row = [&](Rows x, int c, int gr) { return c < min(p.tokens, c_hi - x.c) && x.g + gr < a.G; };
+    // (where the lane's rows are from the tile's first one on; near where 31 bits
+    // hold that, which saves registers)
+    int q_off[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int row = wave * (kRows / kWaves) + i * RPI + lane / RC;
-      q_off[i] = (row / per * a.q.ld_tok + row % per * a.q.ld_head) * 2;
+      const int c = token_of(row);
+      q_off[i] = (int)((c * a.q.ld_tok + (row - c * per) * a.q.ld_head) * 2) + lane % RC * 16;
     }
-    auto stage = [&](int t, int buf) {
-      const char* base = a.q.base + (b * a.q.ld_seq + c_of(t) * a.q.ld_tok + (h * a.G + g_of(t)) * a.q.ld_head) * 2;
-      const bool whole = p.tokens * per == kRows && c_hi - c_of(t) >= p.tokens && a.G - g_of(t) >= per;
+    // A tile's rows pass through registers: LDS that loads fill by themselves would
+    // be read only when they have all arrived, the next tile's among them.
+    u32x4 raw[NI];
+    auto fetch = [&](Rows x) {
+      const char* base = a.q.base + (b * a.q.ld_seq + x.c * a.q.ld_tok + (h * a.G + x.g) * a.q.ld_head) * 2;
+      const bool plain = p.near && whole(x);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
-        const int first = wave * (kRows / kWaves) + i * RPI;
-        const int row = first + lane / RC;
-        int64_t off = q_off[i];
-        if (!whole && !has_row(t, row)) off = 0;  // (stands for a row that is there)
-        __builtin_amdgcn_global_load_lds(
-            (const __attribute__((address_space(1))) uint32_t*)(base + off + row_chunk<D>(row, lane % RC) * 16),
-            (__attribute__((address_space(3))) uint32_t*)(s_q[buf] + first * D * 2), 16, 0, 0);
+        int64_t off = (uint32_t)q_off[i];
+        if (!plain) {
+          __builtin_amdgcn_sched_barrier(0);
+          const int row = wave * (kRows / kWaves) + i * RPI + lane / RC, c = token_of(row), gr = row - c * per;
+          off = lane % RC * 16;
+          if (has_row(x, c, gr)) off += (c * a.q.ld_tok + gr * a.q.ld_head) * 2;  // (else another stands for it)
+        }
+        raw[i] = *reinterpret_cast<const u32x4*>(base + off);
       }
     };
-    // Minus the lane's rows' log-sums; minus infinity where there is no row.
-    int64_t lse_off[2];
+    auto store = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) lse_off[i] = (int64_t)((32 * i + n) % per) * g.C + (32 * i + n) / per;
-    auto load_lse = [&](int t, float (&neg)[2]) {
-      const float* base = a.lse + ((int64_t)b * a.heads + h * a.G + g_of(t)) * g.C + c_of(t);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bool there = has_row(t, 32 * i + n);
-        const float lse = base[there ? lse_off[i] : 0];
-        neg[i] = there ? -lse_of_weights(lse * kLog2e) : kNegInf;
+      for (int i = 0; i < NI; ++i) {
+        const int row = wave * (kRows / kWaves) + i * RPI + lane / RC;
+        *reinterpret_cast<u32x4*>(s_q[buf] + row * D * 2 + row_chunk<D>(row, lane % RC) * 16) = raw[i];
       }
     };
-    auto arrived = [&] {
-      asm volatile("" ::: "memory");
-      __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
+    // The rows' log-sums, some of a tile by every wavefront: loaded two tiles ahead,
+    // put to LDS one ahead (and nothing is done with them before, or every tile
+    // waits for its load).
+    constexpr int RW = kRows / kWaves;
+    const int my_row = wave * RW + (lane & (RW - 1)), my_c = token_of(my_row), my_g = my_row - my_c * per;
+    auto load_lse = [&](Rows x) {
+      const float* base = a.lse + ((int64_t)b * a.heads + h * a.G + x.g) * g.C + x.c;
+      return base[has_row(x, my_c, my_g) ? my_g * g.C + my_c : 0];
+    };
+    auto put_lse = [&](Rows x, int buf, float lse) {
+      if (lane < RW) {
+        const bool there = has_row(x, my_c, my_g);
+        s_neg[buf][my_row] = there ? -lse_of_weights(lse * kLog2e) : kNegInf;
+        s_lim[buf][my_row] = there ? old + x.c + my_c + 1 : 0;
+      }
     };
 
     float sum[NB][16];
@@ -148,57 +177,103 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       for (int e = 0; e < 16; ++e) sum[i][e] = 0.f;
     const uint32_t q_base = (uint32_t)(uintptr_t)(lds_char*)&s_q[0][0] + n * D * 2 + row_chunk<D>(n, gh) * 16;
 
+    // Scores of 32 rows on their way to the sums: the matrix instructions of the
+    // next 32 rows are issued between the exponentials of these.  A score x adds
+    // 2^(x * held_scale + held_neg).
+    f32x16 even[NB], odd[NB];
+    float held_scale = 0.f, held_neg = kNegInf;  // (nothing is held yet)
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) odd[i][e] = 0.f;
+    // Scores of the rows at LDS address `at` and, an instruction's share at a
+    // time, the held ones' weights to the sums.
+    auto products = [&](uint32_t at, f32x16 (&s)[NB], const f32x16 (&held)[NB]) {
+      constexpr int EACH = 16 * NB / KS;  // weights a step
+      constexpr int AHEAD = 2;            // steps that operands are read ahead
+      auto read = [&](int k) { return as_bf16x8(*(const lds_u32x4*)(uintptr_t)(at ^ (32 * k))); };
+      bf16x8 q[KS];
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) q[k] = read(k);
+      float x[2][EACH];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        if (k + AHEAD < KS) q[k + AHEAD] = read(k + AHEAD);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+          s[i] = mfma32(kf[i][k], q[k], k ? s[i] : f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+          const int o = k * EACH + u;
+          x[k % 2][u] = exp2_fast(fmaf(held[o / 16][o % 16], held_scale, held_neg));
+        }
+        // (a step later, when they are there)
+        if (k > 0) {
+#pragma unroll
+          for (int u = 0; u < EACH; ++u) sum[((k - 1) * EACH + u) / 16][((k - 1) * EACH + u) % 16] += x[(k - 1) % 2][u];
+        }
+        // (steps stay apart: left to itself the compiler gathers the exponentials
+        // where the sums are next needed)
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int u = 0; u < EACH; ++u) sum[((KS - 1) * EACH + u) / 16][((KS - 1) * EACH + u) % 16] += x[(KS - 1) % 2][u];
+#pragma unroll
+      for (int u = 0; u < 16 * NB; ++u) asm volatile("" : "+v"(sum[u / 16][u % 16]));
+    };
+    auto rows32 = [&](uint32_t at, int buf, int r, bool all, f32x16 (&s)[NB], const f32x16 (&held)[NB]) {
+      products(at, s, held);
+      const float neg = s_neg[buf][32 * r + n];
+      held_scale = a.scale2;
+      held_neg = neg;
+      if (all && !__any(fabsf(neg) > kLargeLse && neg != kNegInf)) return;
+      // Hidden keys, rows whose weights are held to 1: the exponents here, one by
+      // one (all at once they take 60 registers more).
+      const int lim = s_lim[buf][32 * r + n];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const uint32_t mine = ((uint32_t)(ok >> (32 * i)) & below(lim - kw - 32 * i)) >> (4 * gh);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float y = fmaf(s[i][e], a.scale2, neg);
+          s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? (y > 0.f ? 0.f : y) : kNegInf;
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      held_scale = 1.f;
+      held_neg = 0.f;
+    };
+
     if (t0 < t1) {
-      float neg[2], neg_next[2];
-      stage(t0, 0);
-      load_lse(t0, neg);
-      arrived();
+      Rows now = rows_of(t0);
+      fetch(now);
+      put_lse(now, 0, load_lse(now));
+      store(0);
+      Rows next = t0 + 1 < t1 ? after(now) : now;
+      float lse = load_lse(next);
+      __syncthreads();
       int buf = 0;
       for (int t = t0; t < t1; ++t) {
         if (t + 1 < t1) {
-          stage(t + 1, buf ^ 1);
-          load_lse(t + 1, neg_next);
+          put_lse(next, buf ^ 1, lse);
+          fetch(next);
         }
-        const bool all = ok == (NB == 2 ? ~0ull : 0xffffffffull) && old + c_of(t) + 1 >= kw + kKeys;  // every row sees every key
+        const Rows then = t + 2 < t1 ? after(next) : next;
+        lse = load_lse(then);
+        const bool all = ok == kAllKeys && old + now.c + 1 >= kw + kKeys;  // every row sees every key
         const uint32_t at = q_base + buf * (kRows * D * 2);
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          f32x16 s[NB];
-#pragma unroll
-          for (int i = 0; i < NB; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
-#pragma unroll
-          for (int k = 0; k < KS; ++k) {
-            const bf16x8 q = as_bf16x8(*(const lds_u32x4*)(uintptr_t)((at ^ (32 * k)) + r * 64 * D));
-#pragma unroll
-            for (int i = 0; i < NB; ++i) s[i] = mfma32(kf[i][k], q, s[i]);
-          }
-          const bool large = __any(fabsf(neg[r]) > kLargeLse && neg[r] != kNegInf);
-          if (all && !large) {
-#pragma unroll
-            for (int i = 0; i < NB; ++i)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(s[i][e], a.scale2, neg[r]));
-          } else {
-            const int row = 32 * r + n;
-            const int lim = has_row(t, row) ? old + c_of(t) + row / per + 1 : 0;
-#pragma unroll
-            for (int i = 0; i < NB; ++i) {
-              const uint32_t mine = ((uint32_t)(ok >> (32 * i)) & below(lim - kw - 32 * i)) >> (4 * gh);
-#pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float x = weight_of(s[i][e], a.scale2, -neg[r]);
-                sum[i][e] += mine >> (8 * (e / 4) + e % 4) & 1u ? x : 0.f;
-              }
-            }
-          }
-        }
-        neg[0] = neg_next[0];
-        neg[1] = neg_next[1];
+        rows32(at, buf, 0, all, even, odd);
+        rows32(at + 64 * D, buf, 1, all, odd, even);
+        if (t + 1 < t1) store(buf ^ 1);
         buf ^= 1;
-        arrived();
+        now = next;
+        next = then;
+        __syncthreads();
       }
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(odd[i][e], held_scale, held_neg));
     }
 
     // Over the 32 rows' lanes; then key 8(e/4) + 4gh + e%4 of block i is written
@@ -213,6 +288,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
 #pragma unroll
         for (int m = 1; m < 32; m <<= 1) v += __shfl_xor(v, m);
         if (n == e) mine = v;
+        __builtin_amdgcn_sched_barrier(0);
       }
       if (n < 16) out[32 * i + 8 * (n / 4) + 4 * gh + n % 4] = mine;
     }
@@ -257,6 +333,9 @@ WeighPlan weigh_plan(int B, int H, int G, int d, int slots, int watch) {
   p.pieces = (int)std::max<int64_t>(
       1, std::min<int64_t>(std::min<int64_t>(kMaxPieces, row_tiles / 8), 8 * cus / blocks));
   p.ld = (int64_t)tiles * kSlots;
+  const int per = std::min(G, kRows);
+  p.per_inverse = (uint32_t)((65536 + per - 1) / per);
+  p.near = 0;
   p.part = nullptr;
   return p;
 }
@@ -280,6 +359,7 @@ size_t weigh_tile_workspace(int B, int H, int G, int d, int slots, int watch) {
 hipError_t launch_weigh_tile(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s) {
   WeighPlan p = weigh_plan(a.pg.B, a.pg.H, a.G, a.pg.d, a.pg.max_tokens, w.watch);
   p.part = (float*)ws;
+  p.near = ((p.tokens - 1) * a.q.ld_tok + (std::min(a.G, kRows) - 1) * a.q.ld_head + a.pg.d) * 2 < INT32_MAX;
   if (a.pg.d == 64)
     launch_tiles<64>(a, w, p, q4, s);
   else if (a.pg.d == 128)
