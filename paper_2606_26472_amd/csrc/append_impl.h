@@ -22,7 +22,7 @@ __device__ __forceinline__ uint32_t block_byte(uint32_t top_bits) {
 // (kv), four lanes to a block of 32.  A key's partner channels are read again
 // rather than exchanged (they are in the cache), so that every layout and
 // rotary_dim is one code.
-template <bool Q4, int U, class Args>
+template <bool Q4, bool WAVE, int U, class Args>
 __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv, int h, int step,
                                             int vec) {
   const PagedArgs& g = a.pg;
@@ -50,7 +50,7 @@ __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv,
   }
   const int slot = t.n - t.nn + c;
   const int64_t off = row_offset(g, b, slot);
-  auto turns = turns_of(a.rope);
+  auto turns = turns_of<WAVE>(a.rope);
   bool bad = off < 0;
   if (a.rope.table || a.pos) bad |= !turns.find(a.rope, b, c) && a.rope.table;
   if (bad) {
@@ -64,10 +64,12 @@ __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv,
       raise_flag(g.status, b);  // (no place for its id: a step would move one that was never set)
   }
   f32x4 cs[4];
+  if (a.rope.table && __any(rot)) turns.stage(a.rope);
   if (rot) {
-    const int pair = half ? first * 8 : vec * 4;
-    turns.template load<4>(a.rope, pair, cs);
-    if (half) turns.template load<4>(a.rope, pair + 4, cs + 2);
+    if (half)
+      turns.template load<8>(a.rope, first * 8, cs);
+    else
+      turns.template load<4>(a.rope, vec * 4, cs);
   }
   char* row = g.plane[kv] + off;
 #pragma unroll
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(256) void k_append(Args a, int64_t nq_blocks, int p
     const int b = at.token / g.C, c = at.token - b * g.C;
     if (c >= seq_tokens(g, b).nn) return;
     const int iph = g.d / 16, h = at.item / iph;
-    rope_items<false, UQ>(a.q, a.q_out, a.rope, g.status, b, c, h, a.heads / UQ, at.item - h * iph, g.d);
+    rope_items<false, WAVE, UQ>(a.q, a.q_out, a.rope, g.status, b, c, h, a.heads / UQ, at.item - h * iph, g.d);
     return;
   }
   const Place at = place_of<WAVE>(block - nq_blocks, per_kv, tokens);
@@ -135,7 +137,7 @@ __global__ __launch_bounds__(256) void k_append(Args a, int64_t nq_blocks, int p
   const int b = at.token / g.C, c = at.token - b * g.C;
   const int vph = g.d / 8, heads = g.H / UKV;
   const int hv = at.item / vph, kv = hv / heads;
-  append_vecs<Q4, UKV>(a, b, c, kv, hv - kv * heads, heads, at.item - hv * vph);
+  append_vecs<Q4, WAVE, UKV>(a, b, c, kv, hv - kv * heads, heads, at.item - hv * vph);
 }
 
 // Heads a thread takes, of queries as of keys and values: the way to a token's
@@ -150,10 +152,11 @@ void launch_append_heads(const Args& a, hipStream_t s) {
   const int64_t tokens = (int64_t)a.pg.B * a.pg.C;
   const int per_q = a.q.base ? a.heads / UQ * (a.pg.d / 16) : 64;
   const int per_kv = 2 * (a.pg.H / UKV) * (a.pg.d / 8);
-  const int64_t nq = a.q.base ? (tokens * per_q + 255) / 256 : 0;
-  const dim3 grid = linear_grid(nq + (tokens * per_kv + 255) / 256, 256);
-  if (per_q % 64 == 0 && per_kv % 64 == 0)
-    hipLaunchKernelGGL((k_append<Q4, true, UQ, UKV, Args>), grid, dim3(256), 0, s, a, nq, per_q, per_kv);
+  const bool wave = by_wave(a.rope, per_q) && by_wave(a.rope, per_kv);
+  const int64_t nq = a.q.base ? (threads_of(tokens, per_q, wave) + 255) / 256 : 0;
+  const dim3 grid = linear_grid(nq + (threads_of(tokens, per_kv, wave) + 255) / 256, 256);
+  if (wave)
+    hipLaunchKernelGGL((k_append<Q4, true, UQ, UKV, Args>), grid, dim3(256), turns_lds(a.rope), s, a, nq, per_q, per_kv);
   else
     hipLaunchKernelGGL((k_append<Q4, false, UQ, UKV, Args>), grid, dim3(256), 0, s, a, nq, per_q, per_kv);
 }

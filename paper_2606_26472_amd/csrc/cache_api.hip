@@ -48,14 +48,14 @@ int check_axes(const epikv_rope_cfg* r, const epikv_axes* x) {
   return sum == r->rotary_dim / 2 ? EPIKV_OK : EPIKV_EINVAL_SHAPE;
 }
 
-// Every pair's axis and its place there, of checked axes.
-void deal_pairs(const epikv_axes* x, uint8_t (&axis)[512], uint16_t (&place)[512]) {
+// Every pair's place on its axis and how many pairs that has, of checked axes.
+void deal_pairs(const epikv_axes* x, uint16_t (&place)[512], uint16_t (&count)[512]) {
   int used[EPIKV_MAX_AXES] = {0, 0, 0, 0};
   int total = 0, a = 0;
   for (int k = 0; k < x->n_axes; ++k) total += x->pairs[k];
   for (int i = 0; i < total; ++i) {
     while (used[a] == x->pairs[a]) a = (a + 1) % x->n_axes;
-    axis[i] = (uint8_t)a;
+    count[i] = (uint16_t)x->pairs[a];
     place[i] = (uint16_t)used[a]++;
     if (x->order == EPIKV_AXES_TURNS) a = (a + 1) % x->n_axes;
   }
@@ -195,10 +195,27 @@ RopeAxesArg rope_axes_arg(const epikv_rope_cfg* r, const epikv_axes* x, const fl
   RopeAxesArg a = {};
   static_cast<RopeArg&>(a) = rope_arg(r, table, positions, ld_pos, transpose);
   a.n_axes = x->n_axes;
-  uint8_t axis[512];
-  uint16_t place[512];
-  deal_pairs(x, axis, place);
-  for (int i = 0; i < r->rotary_dim / 2; ++i) a.axis[i / 8] |= (uint16_t)(axis[i] << (2 * (i % 8)));
+  // Runs: of one axis each, or of those that still take turns.
+  int left[EPIKV_MAX_AXES], first = 0, n_runs = 0;
+  for (int k = 0; k < x->n_axes; ++k) left[k] = x->pairs[k];
+  for (int k = 0; k < EPIKV_MAX_AXES; ++k) a.start[k] = 1 << 20;
+  while (first < r->rotary_dim / 2) {
+    int turning[EPIKV_MAX_AXES], m = 0, rounds = INT32_MAX;
+    for (int k = 0; k < x->n_axes; ++k)
+      if (left[k] > 0 && (m == 0 || x->order == EPIKV_AXES_TURNS)) {
+        turning[m++] = k;
+        rounds = std::min(rounds, left[k]);
+      }
+    const int run = n_runs++;
+    a.start[run] = first;
+    a.turns[run] = (uint32_t)m;
+    a.inverse[run] = (uint32_t)((65536 + m - 1) / m);
+    // (pair i is turned by turning[(i - first) % m])
+    for (int i = 0; i < 16; ++i)
+      a.axes[run] |= (uint32_t)turning[((i - first) % m + m) % m] << (2 * i);
+    for (int k = 0; k < m; ++k) left[turning[k]] -= rounds;
+    first += m * rounds;
+  }
   return a;
 }
 
@@ -295,9 +312,7 @@ EPIKV_EXPORT int epikv_rope_axes_table(const epikv_rope_cfg* rope, const epikv_a
     return launched(launch_rope_table(table_args(rope, table), stream));
   RopeAxesTableArgs a = {};
   a.t = table_args(rope, table);
-  uint8_t axis[512];
-  deal_pairs(axes, axis, a.place);
-  for (int i = 0; i < a.t.half; ++i) a.count[i] = (uint16_t)axes->pairs[axis[i]];
+  deal_pairs(axes, a.place, a.count);
   return launched(launch_rope_axes_table(a, stream));
 }
 

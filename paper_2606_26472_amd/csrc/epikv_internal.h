@@ -502,7 +502,11 @@ struct RopeAxesArg : RopeArg {
   const int32_t* ids;                      // the tokens' ids, as positions of one axis
   int64_t ld_ids;
   int32_t n_axes;
-  uint16_t axis[64];                       // two bits a pair, eight pairs a word
+  // The pairs in runs, in each of which the same axes take turns: a run's first
+  // pair, how many turn, 2^16 / that (rounded up), and the axes of pairs k,
+  // k + 1, ... from a k that is a multiple of its turns on, two bits each.
+  int32_t start[EPIKV_MAX_AXES];
+  uint32_t turns[EPIKV_MAX_AXES], inverse[EPIKV_MAX_AXES], axes[EPIKV_MAX_AXES];
 };
 
 // Where the tokens are: the layer's two planes, through the page table.

@@ -64,15 +64,16 @@ __global__ __launch_bounds__(256) void k_rope(Args a, int per) {
   const int b = at.token / a.C, c = at.token - b * a.C;
   const int iph = a.d / (FP32 ? 8 : 16);
   const int h = at.item / iph;
-  rope_items<FP32, 1>(a.x, a.y, a.rope, a.status, b, c, h, 0, at.item - h * iph, a.d);
+  rope_items<FP32, WAVE, 1>(a.x, a.y, a.rope, a.status, b, c, h, 0, at.item - h * iph, a.d);
 }
 
 template <bool FP32, class Args>
 hipError_t launch_rope_type(const Args& a, hipStream_t s) {
   const int per = a.heads * (a.d / (FP32 ? 8 : 16));
-  const dim3 grid = linear_grid(((int64_t)a.B * a.C * per + 255) / 256, 256);
-  if (per % 64 == 0)
-    hipLaunchKernelGGL((k_rope<FP32, true, Args>), grid, dim3(256), 0, s, a, per);
+  const bool wave = by_wave(a.rope, per);
+  const dim3 grid = linear_grid((threads_of((int64_t)a.B * a.C, per, wave) + 255) / 256, 256);
+  if (wave)
+    hipLaunchKernelGGL((k_rope<FP32, true, Args>), grid, dim3(256), turns_lds(a.rope), s, a, per);
   else
     hipLaunchKernelGGL((k_rope<FP32, false, Args>), grid, dim3(256), 0, s, a, per);
   return hipGetLastError();

@@ -45,7 +45,9 @@ __device__ __forceinline__ f32x2 pair_of(const f32x4* cs, int i) {
 
 // Where a token's cosines and sines are: the table's row of its position.
 struct TableRow {
+  static constexpr bool STAGED = false;
   int64_t p;
+  __device__ __forceinline__ void stage(const RopeArg&) {}
   // false: the position is out of range
   __device__ __forceinline__ bool find(const RopeArg& r, int b, int c) {
     p = position_of(r, b, c);
@@ -61,9 +63,14 @@ struct TableRow {
 };
 
 // Positions on several axes: every pair is in the row of its axis' position.
-// The rows are read pair by pair, 8 bytes a lane where one position reads 16.
+// WAVE: the wavefront has one token; its pairs come into LDS, one a lane, and
+// from there to the lanes as from a row of the table.  (Pair by pair from the
+// table, eight loads a lane, 16384 tokens of 32 heads of 128 took 66 us.)
+template <bool WAVE>
 struct TableRows {
+  static constexpr bool STAGED = WAVE;
   uint32_t p[EPIKV_MAX_AXES];
+  float2* lds;  // the wavefront's, of r / 2 pairs
   __device__ __forceinline__ bool find(const RopeAxesArg& r, int b, int c) {
     bool in = true;
 #pragma unroll
@@ -76,26 +83,66 @@ struct TableRows {
     }
     return in;
   }
+  // The axes of the eight pairs from i on, two bits each.
+  __device__ __forceinline__ uint32_t axes_at(const RopeAxesArg& r, int i) const {
+    uint32_t word = 0;
+#pragma unroll
+    for (int k = 0; k < EPIKV_MAX_AXES; ++k) {  // (those past the last begin past every pair)
+      const uint32_t at = (uint32_t)i - r.turns[k] * (((uint32_t)i * r.inverse[k]) >> 16);
+      const uint32_t below = (1u << (2 * min(max(r.start[k] - i, 0), 8))) - 1u;  // pairs of the runs before
+      word = (word & below) | (r.axes[k] >> (2 * at) & ~below);
+    }
+    return word;
+  }
+  __device__ __forceinline__ float2 entry(const RopeAxesArg& r, uint32_t axis, int i) const {
+    const uint32_t lo = axis & 1u ? p[1] : p[0], hi = axis & 1u ? p[3] : p[2];
+    return r.table[(uint64_t)(axis & 2u ? hi : lo) * ((uint32_t)r.r / 2) + (uint32_t)i];
+  }
+  // All lanes of the wavefront that have an item (its first ones), before load.
+  __device__ __forceinline__ void stage(const RopeAxesArg& r) {
+    if constexpr (WAVE) {
+      const int lanes = __popcll(__ballot(true));
+      for (int i = threadIdx.x & 63; i < r.r / 2; i += lanes) lds[i] = entry(r, axes_at(r, i), i);
+      wave_sync();
+    }
+  }
   template <int M>
   __device__ __forceinline__ void load(const RopeAxesArg& r, int i, f32x4* cs) const {
-    const uint32_t axes = (uint32_t)r.axis[i >> 3] >> (2 * (i & 7));
-    const uint32_t row = (uint32_t)r.r / 2;
+    if constexpr (WAVE) {
 #pragma unroll
-    for (int k = 0; k < M; ++k) {
-      const uint32_t lo = axes >> (2 * k) & 1u ? p[1] : p[0], hi = axes >> (2 * k) & 1u ? p[3] : p[2];
-      const float2 t = r.table[(uint64_t)(axes >> (2 * k) & 2u ? hi : lo) * row + (uint32_t)(i + k)];
-      cs[k / 2][2 * (k % 2)] = t.x;
-      cs[k / 2][2 * (k % 2) + 1] = t.y;
+      for (int k = 0; k < M / 2; ++k) cs[k] = *reinterpret_cast<const f32x4*>(lds + i + 2 * k);
+    } else {
+      const uint32_t axes = axes_at(r, i);
+#pragma unroll
+      for (int k = 0; k < M; ++k) {
+        const float2 t = entry(r, axes >> (2 * k), i + k);
+        cs[k / 2][2 * (k % 2)] = t.x;
+        cs[k / 2][2 * (k % 2) + 1] = t.y;
+      }
     }
   }
 };
 
-__device__ __forceinline__ TableRow turns_of(const RopeArg&) { return TableRow{}; }
-__device__ __forceinline__ TableRows turns_of(const RopeAxesArg&) { return TableRows{}; }
+// LDS of a workgroup of four wavefronts with a token each.
+inline unsigned turns_lds(const RopeArg&) { return 0; }
+inline unsigned turns_lds(const RopeAxesArg& r) { return 4 * (r.r / 2) * sizeof(float2); }
+
+template <bool WAVE>
+__device__ __forceinline__ TableRow turns_of(const RopeArg&) {
+  return TableRow{};
+}
+template <bool WAVE>
+__device__ __forceinline__ TableRows<WAVE> turns_of(const RopeAxesArg& r) {
+  extern __shared__ __align__(16) float2 s_turns[];
+  TableRows<WAVE> t;
+  t.lds = WAVE ? s_turns + (threadIdx.x >> 6) * (r.r / 2) : nullptr;
+  return t;
+}
 
 // The id of a new token: its position, or where it has several, an input.
 __device__ __forceinline__ int32_t id_of(const RopeArg&, const TableRow& t, int, int) { return (int32_t)t.p; }
-__device__ __forceinline__ int32_t id_of(const RopeAxesArg& r, const TableRows&, int b, int c) {
+template <bool WAVE>
+__device__ __forceinline__ int32_t id_of(const RopeAxesArg& r, const TableRows<WAVE>&, int b, int c) {
   return r.ld_ids ? r.ids[(int64_t)b * r.ld_ids + c] : r.ids[b] + c;
 }
 
@@ -129,7 +176,7 @@ struct Vec {
 // one layout, and in either neighbouring lanes read and write neighbouring
 // vectors, whole lines at a time (32 bytes a lane, past the caches, wrote
 // float32 at a third of the speed).
-template <bool FP32, int U, class Rope>
+template <bool FP32, bool WAVE, int U, class Rope>
 __device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, const Rope& r,
                                            int32_t* status, int b, int c, int h, int step, int it,
                                            int d) {
@@ -147,16 +194,23 @@ __device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, c
     ru[i] = ld_stream(xp + (i * step * x.ld_head + lo) * ES);
     rv[i] = ld_stream(xp + (i * step * x.ld_head + hi) * ES);
   }
-  auto turns = turns_of(r);
-  if (r.table && !turns.find(r, b, c)) {
-    raise_flag(status, b);
-    return;
+  auto turns = turns_of<WAVE>(r);
+  if (r.table) {
+    if (!turns.find(r, b, c)) {
+      raise_flag(status, b);
+      return;
+    }
+    turns.stage(r);
   }
   f32x4 cs[N / 2];
   if (rot) {
     // (N pairs together, or half of them for each vector)
-    turns.template load<N / 2>(r, r.interleaved ? lo / 2 : lo, cs);
-    turns.template load<N / 2>(r, r.interleaved ? hi / 2 : lo + N / 2, cs + N / 4);
+    if (r.interleaved) {
+      turns.template load<N / 2>(r, lo / 2, cs);
+      turns.template load<N / 2>(r, hi / 2, cs + N / 4);
+    } else {
+      turns.template load<N>(r, lo, cs);
+    }
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
@@ -180,9 +234,9 @@ __device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, c
   }
 }
 
-// Threads over (token, item): `per` items a token.  Where they are a multiple
-// of the wavefront, a wavefront has one token, and what belongs to the token
-// stays in scalar registers.
+// Threads over (token, item): `per` items a token.  With WAVE a wavefront has one
+// token (its last wavefront perhaps fewer items than lanes), and what belongs to
+// the token stays in scalar registers.
 struct Place {
   int token, item;
   bool in;
@@ -192,7 +246,7 @@ template <bool WAVE>
 __device__ __forceinline__ Place place_of(int64_t block, int per, int64_t tokens) {
   Place p;
   if constexpr (WAVE) {
-    const uint32_t waves = (uint32_t)per / 64u;
+    const uint32_t waves = ((uint32_t)per + 63u) / 64u;
     const uint32_t w = (uint32_t)__builtin_amdgcn_readfirstlane((int)(block * 4 + (threadIdx.x >> 6)));
     p.token = (int)(w / waves);
     p.item = (int)(w - (uint32_t)p.token * waves) * 64 + (int)(threadIdx.x & 63);
@@ -201,9 +255,18 @@ __device__ __forceinline__ Place place_of(int64_t block, int per, int64_t tokens
     p.token = (int)(t / (uint32_t)per);
     p.item = (int)(t - (uint32_t)p.token * (uint32_t)per);
   }
-  p.in = p.token < tokens;
+  p.in = p.token < tokens && (!WAVE || p.item < per);
   return p;
 }
+
+// Whether a token's items go to wavefronts of their own: where they fill them,
+// and with positions on several axes (whose turns come through LDS then) where
+// more than half of the lanes have one.  Tokens of 24 heads of 64, 96 items: 37 us
+// so, 60 without; of 9, 36 items: 23, 38; of 5, 20 items: 37, 35; appended with 32
+// items of queries and 32 of keys and values: 71, 62.
+inline bool by_wave(const RopeArg&, int per) { return per % 64 == 0; }
+inline bool by_wave(const RopeAxesArg&, int per) { return 2 * per > (per + 63) / 64 * 64; }
+inline int64_t threads_of(int64_t tokens, int per, bool wave) { return tokens * (wave ? (per + 63) / 64 * 64 : per); }
 
 // Threads beyond 2^32 do not fit place_of's numbers.
 inline bool threads_fit(int64_t tokens, int per) { return tokens * per < ((int64_t)1 << 32) - 256; }

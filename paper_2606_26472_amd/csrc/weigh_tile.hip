@@ -295,26 +295,50 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
   }
 }
 
-// The partial sums of a slot, in order, on what is kept of the old one.
+// The partial sums of a slot, in a fixed order, on what is kept of the old one:
+// four slots a lane, a workgroup's wavefronts taking turns over the partial sums,
+// four on their way at a time.  Bound by latency (16384 slots of 32 partial sums
+// 13 us with a thread for a slot's).
 __global__ __launch_bounds__(256) void k_weigh_reduce(AttendArgs a, WeighArgs w, WeighPlan p, int blocks) {
+  constexpr int SLOTS = 256, AHEAD = 4;
+  __shared__ f32x4 s_sum[4][SLOTS / 4];
   const PagedArgs& g = a.pg;
   const int64_t id = linear_block();
   const int b = (int)(id / blocks);
   if (b >= g.B) return;
   const SeqTokens t = seq_tokens(g, b);
   if (t.nn == 0) return;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int n_part = p.pieces * g.H;
-  for (int64_t j = (id % blocks) * 256 + threadIdx.x; j < t.n; j += (int64_t)blocks * 256) {
-    if (j >= w.ld_s) {
-      raise_flag(g.status, b);
-      return;
+  for (int64_t j0 = (id % blocks) * SLOTS; j0 < t.n; j0 += (int64_t)blocks * SLOTS) {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (j0 + 4 * lane < p.ld) {
+      const float* part = p.part + (int64_t)b * g.H * p.ld + j0 + 4 * lane;
+      for (int i = wave; i < n_part; i += 4 * AHEAD) {
+        f32x4 x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+          const int k = i + 4 * u, piece = k / g.H;
+          x[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if (k < n_part)
+            x[u] = *reinterpret_cast<const f32x4*>(part + ((int64_t)piece * g.B * g.H + (k - piece * g.H)) * p.ld);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) sum += x[u];
+      }
     }
-    float sum = 0.f;
-    for (int i = 0; i < n_part; ++i) {
-      const int piece = i / g.H, h = i - piece * g.H;
-      sum += p.part[(((int64_t)piece * g.B + b) * g.H + h) * p.ld + j];
+    s_sum[wave][lane] = sum;
+    __syncthreads();
+    const int64_t j = j0 + threadIdx.x;
+    if (j < t.n) {
+      const int v = threadIdx.x / 4, e = threadIdx.x % 4;
+      if (j < w.ld_s)
+        write_sum(w, b, (int)j, t, (s_sum[0][v][e] + s_sum[1][v][e]) + (s_sum[2][v][e] + s_sum[3][v][e]));
+      else
+        raise_flag(g.status, b);
     }
-    write_sum(w, b, (int)j, t, sum);
+    __syncthreads();
   }
 }
 
