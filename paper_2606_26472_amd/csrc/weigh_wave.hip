@@ -14,84 +14,96 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWeighSlots = 256;   // of a workgroup, four to a lane
 constexpr int kWeighRows = 512;    // rows whose log-sums a workgroup holds at a time
 constexpr int kMaxTiles = 16384;   // workgroups, about; each goes on to further slots
-constexpr int kRowThreads = 8;     // that read a row's shares
 
 struct WeighScratch {
   float lse[kWeighRows];                       // base 2
   __attribute__((aligned(16))) float sums[8][kWeighSlots];
 };
 
+// The log-sum of one row from its shares, by `lanes` lanes that each take some.
+__device__ __forceinline__ float lse_of_shares(const AttendArgs& a, const WavePlan& p, int b, int h, int r,
+                                               int2 place, int part, int lanes) {
+  constexpr int AHEAD = 8;
+  const int64_t from = ((int64_t)(place.x + b) * a.pg.H + h) * a.R + r, step = (int64_t)a.pg.H * a.R;
+  float top = kNegInf, s = 0.f;
+  for (int k = part; k < place.y; k += AHEAD * lanes) {
+    float2 ml[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ml[u] = p.part_ml[from + min(k + u * lanes, place.y - 1) * step];
+    float grown = top;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) grown = fmaxf(grown, ml[u].x);
+    const float base2 = grown == kNegInf ? 0.f : grown;
+    s *= exp2_fast(top - base2);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) s += k + u * lanes < place.y ? ml[u].y * exp2_fast(ml[u].x - base2) : 0.f;
+    top = grown;
+  }
+  for (int m = 1; m < lanes; m <<= 1) {
+    const float top2 = __shfl_xor(top, m), s2 = __shfl_xor(s, m);
+    const float grown = fmaxf(top, top2);
+    const float base2 = grown == kNegInf ? 0.f : grown;
+    s = s * exp2_fast(top - base2) + s2 * exp2_fast(top2 - base2);
+    top = grown;
+  }
+  return top + __builtin_amdgcn_logf(s);
+}
+
+// The sums of 256 slots, four to a lane, a workgroup's wavefronts taking turns
+// over the counted rows.  SHARES: the rows' log-sums are made from their shares
+// here; else they are in a.lse.
+template <bool SHARES>
 __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, int b,
                                             int tile, const SeqTokens& t, WeighScratch& lds) {
+  constexpr int AHEAD = 8;
   const PagedArgs& g = a.pg;
   const int j0 = tile * kWeighSlots;
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int first = max(0, t.nn - w.watch) * a.G;      // rows of a KV head that count: [first, nn * G)
   const int per_head = t.nn * a.G - first, rows = per_head * g.H;
-  const int2 place = p.split ? p.shares[b] : make_int2(0, 1);
+  const int2 place = SHARES ? p.shares[b] : make_int2(0, 1);
   const int j = j0 + 4 * lane;
   const bool some = j < t.n;  // (scores are there to the end of a unit)
   const float* kept = p.kept + p.kept_at(b, 0, j / kUnit, a.G, g.H) + j % kUnit;
   const int64_t per_kv_head = p.kept_at(0, 1, 0, a.G, g.H);
+  auto lse_at = [&](int h, int r) {
+    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+    return a.lse[((int64_t)b * a.heads + hq) * g.C + c] * kLog2e;
+  };
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int at = 0; at < rows; at += kWeighRows) {
-    const int n = min(kWeighRows, rows - at);
-    if (at) __syncthreads();
-    for (int i = threadIdx.x / kRowThreads; i < n; i += blockDim.x / kRowThreads) {
-      const int h = (at + i) / per_head, r = first + (at + i) - h * per_head;
-      const int part = threadIdx.x % kRowThreads;
-      float lse;
-      if (place.y == 1) {  // whole: the walk wrote it
-        const int c = r / a.G, hq = h * a.G + (r - c * a.G);
-        lse = a.lse[((int64_t)b * a.heads + hq) * g.C + c] * kLog2e;
-      } else {
-        const int64_t from = ((int64_t)(place.x + b) * g.H + h) * a.R + r, step = (int64_t)g.H * a.R;
-        float top = kNegInf, s = 0.f;
-        for (int k = part; k < place.y; k += 4 * kRowThreads) {
-          float2 ml[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u)
-            ml[u] = p.part_ml[from + min(k + u * kRowThreads, place.y - 1) * step];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            if (k + u * kRowThreads >= place.y) continue;
-            const float grown = fmaxf(top, ml[u].x);
-            const float base2 = grown == kNegInf ? 0.f : grown;
-            s = s * exp2_fast(top - base2) + ml[u].y * exp2_fast(ml[u].x - base2);
-            top = grown;
-          }
-        }
-#pragma unroll
-        for (int m = 1; m < kRowThreads; m <<= 1) {
-          const float top2 = __shfl_xor(top, m), s2 = __shfl_xor(s, m);
-          const float grown = fmaxf(top, top2);
-          const float base2 = grown == kNegInf ? 0.f : grown;
-          s = s * exp2_fast(top - base2) + s2 * exp2_fast(top2 - base2);
-          top = grown;
-        }
-        lse = top + __builtin_amdgcn_logf(s);
+  for (int at = 0; at < rows; at += SHARES ? kWeighRows : rows) {
+    const int n = SHARES ? min(kWeighRows, rows - at) : rows;
+    if constexpr (SHARES) {
+      // (as many lanes to a row as the rows leave each, a power of two)
+      int lanes = 1;
+      while (lanes < 64 && 2 * lanes * min(rows, kWeighRows) <= (int)blockDim.x) lanes *= 2;
+      if (at) __syncthreads();
+      for (int i = threadIdx.x / lanes; i < n; i += blockDim.x / lanes) {
+        const int h = (at + i) / per_head, r = first + (at + i) - h * per_head;
+        const int part = threadIdx.x & (lanes - 1);
+        // (whole: the walk wrote it)
+        const float lse = place.y == 1 ? lse_at(h, r) : lse_of_shares(a, p, b, h, r, place, part, lanes);
+        if (part == 0) lds.lse[i] = lse_of_weights(lse);
       }
-      if (part == 0) lds.lse[i] = lse_of_weights(lse);
+      __syncthreads();
     }
-    __syncthreads();
-    if (!some) continue;
-    constexpr int AHEAD = 8;
     for (int i = wave; i < n; i += AHEAD * waves) {
       f32x4 x[AHEAD];
+      float lse[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const int q = at + min(i + u * waves, n - 1);
-        const int h = q / per_head;
-        x[u] = *reinterpret_cast<const f32x4*>(kept + h * per_kv_head + (q - h * per_head) * kUnit);
+        const int k = min(i + u * waves, n - 1), h = (at + k) / per_head, r = at + k - h * per_head;
+        if (some) x[u] = *reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit);
+        lse[u] = SHARES ? lds.lse[k] : lse_at(h, first + r);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         if (i + u * waves >= n) continue;
-        const float lse = lds.lse[i + u * waves];
+        const float l = SHARES ? lse[u] : lse_of_weights(lse[u]);
         // (a slot that the row does not see has -infinity, whatever its log-sum)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += x[u][e] == kNegInf ? 0.f : weight_of(x[u][e], a.scale2, lse);
+        for (int e = 0; e < 4; ++e) sum[e] += x[u][e] == kNegInf ? 0.f : weight_of(x[u][e], a.scale2, l);
       }
     }
   }
@@ -109,6 +121,20 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
   }
 }
 
+template <bool SHARES>
+__device__ __forceinline__ void weigh_tiles(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, int64_t block,
+                                            int tiles, WeighScratch& lds) {
+  const int64_t b = block / tiles;
+  if (b >= a.pg.B) return;
+  const SeqTokens t = seq_tokens(a.pg, (int)b);
+  if (t.nn == 0) return;
+  // (a table may cover far more than the sequence holds)
+  for (int tile = (int)(block - b * tiles); (int64_t)tile * kWeighSlots < t.n; tile += tiles) {
+    weigh_slots<SHARES>(a, p, w, (int)b, tile, t, lds);
+    __syncthreads();
+  }
+}
+
 // Workgroups of the join, then those of the sums: both need what the walk left
 // and nothing of each other.
 template <int D>
@@ -118,34 +144,44 @@ __global__ __launch_bounds__(512) void k_join_weigh(AttendArgs a, WavePlan p, We
     WeighScratch weigh;
   } lds;
   const int64_t block = linear_block();
-  if (block < n_join) {
+  if (block < n_join)
     join_row<D>(a, p, block, lds.join);
-    return;
-  }
-  const int64_t at = block - n_join, b = at / tiles;
-  if (b >= a.pg.B) return;
-  const SeqTokens t = seq_tokens(a.pg, (int)b);
-  if (t.nn == 0) return;
-  // (a table may cover far more than the sequence holds)
-  for (int tile = (int)(at - b * tiles); (int64_t)tile * kWeighSlots < t.n; tile += tiles) {
-    weigh_slots(a, p, w, (int)b, tile, t, lds.weigh);
-    __syncthreads();
-  }
+  else
+    weigh_tiles<true>(a, p, w, block - n_join, tiles, lds.weigh);
+}
+
+// The sums alone, after a join that leaves every row's log-sum in a.lse.
+__global__ __launch_bounds__(256) void k_weigh(AttendArgs a, WavePlan p, WeighArgs w, int tiles) {
+  __shared__ WeighScratch lds;
+  weigh_tiles<false>(a, p, w, linear_block(), tiles, lds);
 }
 
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 int units_in(int slots) { return (slots + kUnit - 1) / kUnit; }
 
+// Tiles of all sequences up to which their log-sums are made beside the join, in
+// every tile's workgroup anew; more wait for it.  A launch less against that work:
+// MERGE_NOTE
+constexpr int kMergeTiles = 256;
+
 template <int D>
 hipError_t launch_weigh(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, bool q4, hipStream_t s) {
-  const hipError_t e = launch_shares<D, true>(a, p, q4, s);
+  hipError_t e = launch_shares<D, true>(a, p, q4, s);
   if (e != hipSuccess) return e;
-  const int waves = p.split ? join_waves(p, a.pg.B) : 4;
-  const int tiles = std::min((a.pg.max_tokens + kWeighSlots - 1) / kWeighSlots, std::max(1, kMaxTiles / a.pg.B));
-  const int64_t n_join = p.split ? (int64_t)a.pg.B * a.pg.H * a.R : 0;
-  hipLaunchKernelGGL(k_join_weigh<D>, linear_grid(n_join + (int64_t)a.pg.B * tiles, waves * 64), dim3(waves * 64), 0, s,
-                     a, p, w, n_join, tiles);
+  const int all_tiles = (a.pg.max_tokens + kWeighSlots - 1) / kWeighSlots;
+  const int tiles = std::min(all_tiles, std::max(1, kMaxTiles / a.pg.B));
+  const int64_t blocks = (int64_t)a.pg.B * tiles;
+  const bool merge = p.split && (int64_t)a.pg.B * all_tiles <= kMergeTiles;
+  if (p.split) {
+    const int waves = join_waves(p, a.pg.B);
+    const int64_t n_join = (int64_t)a.pg.B * a.pg.H * a.R;
+    hipLaunchKernelGGL(k_join_weigh<D>, linear_grid(n_join + (merge ? blocks : 0), waves * 64), dim3(waves * 64), 0, s, a,
+                       p, w, n_join, tiles);
+    e = hipGetLastError();
+    if (e != hipSuccess || merge) return e;
+  }
+  hipLaunchKernelGGL(k_weigh, linear_grid(blocks, 256), dim3(256), 0, s, a, p, w, tiles);
   return hipGetLastError();
 }
 
