@@ -198,7 +198,11 @@ RopeAxesArg rope_axes_arg(const epikv_rope_cfg* r, const epikv_axes* x, const fl
   // Runs: of one axis each, or of those that still take turns.
   int left[EPIKV_MAX_AXES], first = 0, n_runs = 0;
   for (int k = 0; k < x->n_axes; ++k) left[k] = x->pairs[k];
-  for (int k = 0; k < EPIKV_MAX_AXES; ++k) a.start[k] = 1 << 20;
+  for (int k = 0; k < EPIKV_MAX_AXES; ++k) {  // (runs past the last: past every pair)
+    a.start[k] = 1 << 20;
+    a.turns[k] = 1;
+    a.inverse[k] = 65536;
+  }
   while (first < r->rotary_dim / 2) {
     int turning[EPIKV_MAX_AXES], m = 0, rounds = INT32_MAX;
     for (int k = 0; k < x->n_axes; ++k)

@@ -24,7 +24,7 @@ constexpr int kWaves = 4;
 constexpr int key_blocks(int d) { return d == 256 ? 1 : 2; }
 constexpr int slots_of_group(int d) { return kWaves * 32 * key_blocks(d); }
 constexpr int kRows = 64;                  // query rows of a tile, at most
-constexpr int kMaxPieces = 16;
+constexpr int kMaxPieces = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLargeLse = 4194304.f;     // from 2^22 on weights are held to 1 one by one
 
@@ -39,6 +39,18 @@ struct WeighPlan {
   int64_t ld;            // of a row of partial sums
   float* part;           // [pieces][B][H][ld]
 };
+
+// The sum over the 32 lanes of a half, on each of them (by register moves: as
+// shuffles the 32 sums of a wavefront took 7 us of every workgroup's time).
+__device__ __forceinline__ float half_sum(float v) {
+  const uint32_t w = __float_as_uint(v);
+  const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  v += dpp_move<0x128>(v);                   // row_ror:8
+  v += dpp_move<0x1B>(dpp_move<0x141>(v));   // row_half_mirror, quad_perm [3,2,1,0]: ^ 4
+  v += dpp_move<0x4E>(v);                    // quad_perm [2,3,0,1]
+  return v + dpp_move<0xB1>(v);              // quad_perm [1,0,3,2]
+}
 
 template <int D, bool Q4>
 __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
@@ -284,11 +296,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       float mine = 0.f;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        float v = sum[i][e];
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) v += __shfl_xor(v, m);
+        const float v = half_sum(sum[i][e]);
         if (n == e) mine = v;
-        __builtin_amdgcn_sched_barrier(0);
       }
       if (n < 16) out[32 * i + 8 * (n / 4) + 4 * gh + n % 4] = mine;
     }
@@ -354,8 +363,13 @@ WeighPlan weigh_plan(int B, int H, int G, int d, int slots, int watch) {
   p.head_tiles = (G + kRows - 1) / kRows;
   const int64_t row_tiles = (int64_t)((watch + p.tokens - 1) / p.tokens) * p.head_tiles;
   const int64_t blocks = (int64_t)B * H * p.slot_tiles;
+  // Pieces: of two tiles at least while they give every compute unit its two
+  // workgroups, of eight where there are more (what a workgroup takes to begin and
+  // to end is worth about two).  512 tokens alone 65 us in pieces of eight, 53 of
+  // two; 4 chunks of 100 over 4096 slots 101 us in pieces of two, 90 in one.
+  const auto pieces = [&](int64_t least, int64_t most) { return std::min(row_tiles / least, most / blocks); };
   p.pieces = (int)std::max<int64_t>(
-      1, std::min<int64_t>(std::min<int64_t>(kMaxPieces, row_tiles / 8), 8 * cus / blocks));
+      1, std::min<int64_t>(kMaxPieces, std::max(pieces(2, 2 * cus), pieces(8, 8 * cus))));
   p.ld = (int64_t)tiles * kSlots;
   const int per = std::min(G, kRows);
   p.per_inverse = (uint32_t)((65536 + per - 1) / per);
