@@ -867,17 +867,20 @@ size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, i
  *                   all query heads h of exp(scale*(q . k_j) - lse[b][h][c])
  * with keep = keep_old, or keep_new for the new tokens' slots; a sum kept by 0
  * is not read, whatever it holds.  A token adds nothing to slots it does not
- * see, nor where it sees nothing; slots in pages out of range get nothing
- * added.  Entries from n_cached[b] on are left as they are, and so is a
- * sequence without new tokens or with counts out of range; a slot >= ld_s has
- * no place (not written; flags the sequence).  Weights and sums are float32,
- * added in a fixed order; of a token whose largest score passes 2^30, where
- * float32 no longer tells scores apart, nothing may be added.
+ * see, and a query head of it nothing at all where its log-sum is not finite
+ * (it sees nothing; a NaN or an infinity is among its scores; they pass 2^30,
+ * where float32 no longer tells them apart): one bad token does not spoil sums
+ * that go on.  Slots in pages out of range get nothing added.  Entries from
+ * n_cached[b] on are left as they are, and so is a sequence without new tokens
+ * or with counts out of range; a slot >= ld_s has no place (not written; flags
+ * the sequence).  Weights (1 at most) and sums are float32, added in a fixed
+ * order.
  * The sums are scores of the slots as epikv_select takes them: added up over
  * the layers, they go to epikv_evict_step (chunk = 0, `scores`), which moves
  * them with the rows.
  * weights and old: 4-byte aligned; weights overlaps no other argument but old,
- * which is weights itself or apart from it (EPIKV_EALIAS).  io as for
+ * which is weights itself or apart from it (EPIKV_EALIAS; that neither overlaps
+ * the pool is not checked).  io as for
  * epikv_attend, its workspace of epikv_attend_weigh_workspace_bytes(...); out
  * and lse are those of epikv_attend, bit for bit.
  */

@@ -134,7 +134,8 @@ def attend(q, k, v, n_new, scale, ok=None):
 
 def attend_weights(q, k, n_new, scale, ok=None):
     """w [n_new][Hq][n]: how much every query looks at every slot (softmax
-    over what it sees), arguments as for attend."""
+    over what it sees), arguments as for attend.  A query without a finite
+    log-sum looks at nothing."""
     n, H, d = k.shape
     Hq = q.shape[1]
     w = np.zeros((n_new, Hq, n))
@@ -144,7 +145,7 @@ def attend_weights(q, k, n_new, scale, ok=None):
             see &= ok
         for h in range(Hq):
             s = np.where(see, scale * (k[:, h * H // Hq] @ q[c, h]), -np.inf)
-            if s.max() != -np.inf:  # (NaN goes on)
+            if see.any() and np.isfinite(s.max()):
                 e = np.where(see, np.exp(s - s.max()), 0.0)
                 w[c, h] = e / e.sum()
     return w

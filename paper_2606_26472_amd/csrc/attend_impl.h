@@ -93,17 +93,16 @@ __device__ __forceinline__ int row_chunk(int row, int c) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A log-sum as the weights take it: a row that sees nothing has -infinity (and
-// so has one whose largest score, past 2^30, is less exact than what its
-// exponential can bear); every weight is 0 then.
-__device__ __forceinline__ float lse_of_weights(float lse2) { return lse2 == kNegInf ? -kNegInf : lse2; }
+// Whether a row counts: one that sees nothing, or has a NaN or an infinity among
+// its scores (or scores past 2^30, less exact than their exponentials can bear),
+// has no finite log-sum and adds nothing to any slot, or one token would leave
+// NaN in sums that go on for good.
+__device__ __forceinline__ bool row_counts(float lse) { return fabsf(lse) < -kNegInf; }
 
 // A row's weight of a slot from its score and its log-sum to the base 2.  One
-// at most: what both were rounded to may leave more where they are large.  NaN
-// stays.
+// at most: what both were rounded to may leave more where they are large.
 __device__ __forceinline__ float weight_of(float score, float scale2, float lse2) {
-  const float y = fmaf(score, scale2, -lse2);
-  return exp2_fast(y > 0.f ? 0.f : y);
+  return exp2_fast(fminf(fmaf(score, scale2, -lse2), 0.f));
 }
 
 // A slot's sum: what is kept of the old one and this call's.

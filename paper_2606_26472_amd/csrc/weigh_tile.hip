@@ -62,6 +62,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
   constexpr int NI = kRows / kWaves / RPI;
   __shared__ __align__(1024) char s_q[2][kRows * D * 2];
   __shared__ float s_neg[2][kRows];  // minus a row's log-sum (minus infinity: no such row)
+  constexpr float kNotCounted = -kNegInf;
   __shared__ int s_lim[2][kRows];    // the slots that it sees
   const PagedArgs& g = a.pg;
   const int lane = threadIdx.x & 63;
@@ -89,6 +90,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
 
     bf16x8 kf[NB][KS];
     uint64_t ok = 0;  // which of the wavefront's keys exist
+    bool odd_key = false;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int j = kw + 32 * i + n;
@@ -108,8 +110,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
         }
         if (off < 0) x = u32x4{0, 0, 0, 0};
         kf[i][s] = as_bf16x8(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd_key |= word_not_finite(x[e]);
       }
     }
+    odd_key = __any(odd_key);  // (0 times one of its channels may be NaN)
 
     // A tile's rows: tokens from c on, heads of the group from g on.
     struct Rows {
@@ -149,13 +154,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         int64_t off = (uint32_t)q_off[i];
+        bool there = true;
         if (!plain) {
           __builtin_amdgcn_sched_barrier(0);
           const int row = wave * (kRows / kWaves) + i * RPI + lane / RC, c = token_of(row), gr = row - c * per;
-          off = lane % RC * 16;
-          if (has_row(x, c, gr)) off += (c * a.q.ld_tok + gr * a.q.ld_head) * 2;  // (else another stands for it)
+          off = (c * a.q.ld_tok + gr * a.q.ld_head) * 2 + lane % RC * 16;
+          there = has_row(x, c, gr);
+          raw[i] = u32x4{0, 0, 0, 0};  // (a row that is not there: scores of 0, but with an odd key)
         }
-        raw[i] = *reinterpret_cast<const u32x4*>(base + off);
+        if (there) raw[i] = *reinterpret_cast<const u32x4*>(base + off);
       }
     };
     auto store = [&](int buf) {
@@ -177,8 +184,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     auto put_lse = [&](Rows x, int buf, float lse) {
       if (lane < RW) {
         const bool there = has_row(x, my_c, my_g);
-        s_neg[buf][my_row] = there ? -lse_of_weights(lse * kLog2e) : kNegInf;
-        s_lim[buf][my_row] = there ? old + x.c + my_c + 1 : 0;
+        const bool counts = there && row_counts(lse);
+        s_neg[buf][my_row] = counts ? -lse * kLog2e : there ? kNotCounted : kNegInf;
+        s_lim[buf][my_row] = counts ? old + x.c + my_c + 1 : 0;
       }
     };
 
@@ -238,9 +246,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       const float neg = s_neg[buf][32 * r + n];
       held_scale = a.scale2;
       held_neg = neg;
-      if (all && !__any(fabsf(neg) > kLargeLse && neg != kNegInf)) return;
-      // Hidden keys, rows whose weights are held to 1: the exponents here, one by
-      // one (all at once they take 60 registers more).
+      if (all && !__any(fabsf(neg) > kLargeLse && (odd_key || neg != kNegInf))) return;
+      // Hidden keys, rows that do not count, rows whose weights are held to 1: the
+      // exponents here, one by one (all at once they take 60 registers more).
       const int lim = s_lim[buf][32 * r + n];
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
@@ -248,7 +256,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const float y = fmaf(s[i][e], a.scale2, neg);
-          s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? (y > 0.f ? 0.f : y) : kNegInf;
+          s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? fminf(y, 0.f) : kNegInf;
           __builtin_amdgcn_sched_barrier(0);
         }
       }

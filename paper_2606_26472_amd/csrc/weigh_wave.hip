@@ -84,7 +84,7 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
         const int part = threadIdx.x & (lanes - 1);
         // (whole: the walk wrote it)
         const float lse = place.y == 1 ? lse_at(h, r) : lse_of_shares(a, p, b, h, r, place, part, lanes);
-        if (part == 0) lds.lse[i] = lse_of_weights(lse);
+        if (part == 0) lds.lse[i] = lse;
       }
       __syncthreads();
     }
@@ -100,10 +100,10 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         if (i + u * waves >= n) continue;
-        const float l = SHARES ? lse[u] : lse_of_weights(lse[u]);
-        // (a slot that the row does not see has -infinity, whatever its log-sum)
+        if (!row_counts(lse[u])) continue;
+        // (a slot that the row does not see has -infinity)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += x[u][e] == kNegInf ? 0.f : weight_of(x[u][e], a.scale2, l);
+        for (int e = 0; e < 4; ++e) sum[e] += weight_of(x[u][e], a.scale2, lse[u]);
       }
     }
   }
