@@ -154,21 +154,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         int64_t off = (uint32_t)q_off[i];
-        bool there = true;
         if (!plain) {
           __builtin_amdgcn_sched_barrier(0);
           const int row = wave * (kRows / kWaves) + i * RPI + lane / RC, c = token_of(row), gr = row - c * per;
-          off = (c * a.q.ld_tok + gr * a.q.ld_head) * 2 + lane % RC * 16;
-          there = has_row(x, c, gr);
-          raw[i] = u32x4{0, 0, 0, 0};  // (a row that is not there: scores of 0, but with an odd key)
+          off = lane % RC * 16;
+          if (has_row(x, c, gr)) off += (c * a.q.ld_tok + gr * a.q.ld_head) * 2;  // (else another is read, and not used)
         }
-        if (there) raw[i] = *reinterpret_cast<const u32x4*>(base + off);
+        raw[i] = *reinterpret_cast<const u32x4*>(base + off);
       }
     };
-    auto store = [&](int buf) {
+    auto store = [&](Rows x, int buf) {
+      const bool all = whole(x);
 #pragma unroll
       for (int i = 0; i < NI; ++i) {
         const int row = wave * (kRows / kWaves) + i * RPI + lane / RC;
+        // (a row that is not there: scores of 0, but with an odd key)
+        if (!all && !has_row(x, token_of(row), row - token_of(row) * per)) raw[i] = u32x4{0, 0, 0, 0};
         *reinterpret_cast<u32x4*>(s_q[buf] + row * D * 2 + row_chunk<D>(row, lane % RC) * 16) = raw[i];
       }
     };
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       Rows now = rows_of(t0);
       fetch(now);
       put_lse(now, 0, load_lse(now));
-      store(0);
+      store(now, 0);
       Rows next = t0 + 1 < t1 ? after(now) : now;
       float lse = load_lse(next);
       __syncthreads();
@@ -284,7 +285,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
         const uint32_t at = q_base + buf * (kRows * D * 2);
         rows32(at, buf, 0, all, even, odd);
         rows32(at + 64 * D, buf, 1, all, odd, even);
-        if (t + 1 < t1) store(buf ^ 1);
+        if (t + 1 < t1) store(next, buf ^ 1);
         buf ^= 1;
         now = next;
         next = then;
