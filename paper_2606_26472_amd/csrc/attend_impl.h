@@ -105,12 +105,13 @@ __device__ __forceinline__ float weight_of(float score, float scale2, float lse2
   return exp2_fast(fminf(fmaf(score, scale2, -lse2), 0.f));
 }
 
-// A slot's sum: what is kept of the old one and this call's.
-__device__ __forceinline__ void write_sum(const WeighArgs& w, int b, int j, const SeqTokens& t, float sum) {
-  const int64_t at = (int64_t)b * w.ld_s + j;
+// A slot's sum: what is kept of the old one and this call's.  j < ld_s.
+__device__ __forceinline__ float kept_sum(const WeighArgs& w, int b, int64_t j, const SeqTokens& t) {
   const float keep = j < t.n - t.nn ? w.keep_old : w.keep_new;
-  const float kept = keep != 0.f ? keep * w.old[at] : 0.f;  // (kept by 0: not read)
-  w.weights[at] = fmaf(w.gain, sum, kept);
+  return keep != 0.f ? keep * w.old[b * w.ld_s + j] : 0.f;  // (kept by 0: not read)
+}
+__device__ __forceinline__ void write_sum(const WeighArgs& w, int b, int64_t j, float kept, float sum) {
+  w.weights[b * w.ld_s + j] = fmaf(w.gain, sum, kept);
 }
 
 // Query rows per KV head up to which the wavefront kernel is taken: the columns

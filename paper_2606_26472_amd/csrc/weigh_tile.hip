@@ -330,6 +330,8 @@ __global__ __launch_bounds__(256) void k_weigh_reduce(AttendArgs a, WeighArgs w,
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int n_part = p.pieces * g.H;
   for (int64_t j0 = (id % blocks) * SLOTS; j0 < t.n; j0 += (int64_t)blocks * SLOTS) {
+    const int64_t j = j0 + threadIdx.x;
+    const float old_sum = j < t.n && j < w.ld_s ? kept_sum(w, b, j, t) : 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     if (j0 + 4 * lane < p.ld) {
       const float* part = p.part + (int64_t)b * g.H * p.ld + j0 + 4 * lane;
@@ -348,11 +350,10 @@ __global__ __launch_bounds__(256) void k_weigh_reduce(AttendArgs a, WeighArgs w,
     }
     s_sum[wave][lane] = sum;
     __syncthreads();
-    const int64_t j = j0 + threadIdx.x;
     if (j < t.n) {
       const int v = threadIdx.x / 4, e = threadIdx.x % 4;
       if (j < w.ld_s)
-        write_sum(w, b, (int)j, t, (s_sum[0][v][e] + s_sum[1][v][e]) + (s_sum[2][v][e] + s_sum[3][v][e]));
+        write_sum(w, b, j, old_sum, (s_sum[0][v][e] + s_sum[1][v][e]) + (s_sum[2][v][e] + s_sum[3][v][e]));
       else
         raise_flag(g.status, b);
     }

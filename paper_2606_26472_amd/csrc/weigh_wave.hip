@@ -71,6 +71,11 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
     const int c = r / a.G, hq = h * a.G + (r - c * a.G);
     return a.lse[((int64_t)b * a.heads + hq) * g.C + c] * kLog2e;
   };
+  // (a workgroup has a thread for every slot; the old sum is on its way meanwhile)
+  const bool live = threadIdx.x < kWeighSlots && j0 + (int)threadIdx.x < t.n;
+  const bool mine = live && j0 + (int)threadIdx.x < w.ld_s;
+  if (live && !mine) raise_flag(g.status, b);
+  const float kept_old = mine ? kept_sum(w, b, j0 + (int)threadIdx.x, t) : 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
   for (int at = 0; at < rows; at += SHARES ? kWeighRows : rows) {
     const int n = SHARES ? min(kWeighRows, rows - at) : rows;
@@ -100,24 +105,23 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         if (i + u * waves >= n) continue;
-        if (!row_counts(lse[u])) continue;
-        // (a slot that the row does not see has -infinity)
+        // (a slot that the row does not see has -infinity.  No branch over rows that
+        // do not count: one sequence of 4224 slots 16.1 us so, 17.4 with it)
+        const bool counts = row_counts(lse[u]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += weight_of(x[u][e], a.scale2, lse[u]);
+        for (int e = 0; e < 4; ++e) {
+          const float y = weight_of(x[u][e], a.scale2, lse[u]);
+          sum[e] += counts ? y : 0.f;
+        }
       }
     }
   }
   *reinterpret_cast<f32x4*>(&lds.sums[wave][4 * lane]) = sum;
   __syncthreads();
-  for (int i = threadIdx.x; i < kWeighSlots; i += blockDim.x) {
-    if (j0 + i >= t.n) continue;
-    if (j0 + i >= w.ld_s) {
-      raise_flag(g.status, b);
-      continue;
-    }
+  if (mine) {
     float y = 0.f;
-    for (int k = 0; k < waves; ++k) y += lds.sums[k][i];
-    write_sum(w, b, j0 + i, t, y);
+    for (int k = 0; k < waves; ++k) y += lds.sums[k][threadIdx.x];
+    write_sum(w, b, j0 + (int)threadIdx.x, kept_old, y);
   }
 }
 
