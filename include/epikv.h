@@ -873,8 +873,7 @@ size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, i
  * that go on.  Slots in pages out of range get nothing added.  Entries from
  * n_cached[b] on are left as they are, and so is a sequence without new tokens
  * or with counts out of range; a slot >= ld_s has no place (not written; flags
- * the sequence).  Weights (1 at most) and sums are float32, added in a fixed
- * order.
+ * the sequence).  Weights and sums are float32, added in a fixed order.
  * The sums are scores of the slots as epikv_select takes them: added up over
  * the layers, they go to epikv_evict_step (chunk = 0, `scores`), which moves
  * them with the rows.

@@ -2,13 +2,13 @@
 // the attention itself.
 //
 // A row's weights need its log-sum, which is known when the attention ends, so
-// the scores are made a second time: a wavefront keeps 64 keys (32 of 256 channels)
-// of a KV head in registers as the first operand of v_mfma 32x32x16 and the query rows stream
-// past through LDS, 64 at a time and two tiles deep.  S^T = K Q^T, in the
-// attention's order of channels (the same scores, bit for bit): lane (n, g) =
-// (lane % 32, lane / 32) has query row n's scores of keys 8i + 4g + 0..3, so a
-// row's log-sum is one register a lane, and a key's sum stays in one register
-// a lane from the first row to the last.  Only then do lanes meet.
+// the scores are made a second time: a wavefront keeps 64 keys (32 of 256
+// channels) of a KV head in registers, as the first operand of v_mfma 32x32x16,
+// and the query rows stream past through LDS, 64 at a time and two tiles deep.
+// S^T = K Q^T, in the attention's order of channels (the same scores, bit for
+// bit): lane (n, g) = (lane % 32, lane / 32) has query row n's scores of keys
+// 8i + 4g + 0..3, so a row's log-sum is one register a lane, and a key's sum stays
+// in one register a lane from the first row to the last.  Only then do lanes meet.
 #include <type_traits>
 
 #include "attend_impl.h"
@@ -26,7 +26,7 @@ constexpr int slots_of_group(int d) { return kWaves * 32 * key_blocks(d); }
 constexpr int kRows = 64;                  // query rows of a tile, at most
 constexpr int kMaxPieces = 64;
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLargeLse = 4194304.f;     // from 2^22 on weights are held to 1 one by one
+constexpr float kLargeLse = 65536.f;       // from 2^16 on weights are held to 1 one by one
 
 // How the work is dealt out: the slots of every (sequence, KV head) in tiles,
 // each tile's rows in `pieces`.
@@ -88,34 +88,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     const int tiles = c_lo < c_hi ? (c_hi - c_lo + p.tokens - 1) / p.tokens * p.head_tiles : 0;
     const int t0 = (int)((int64_t)tiles * piece / p.pieces), t1 = (int)((int64_t)tiles * (piece + 1) / p.pieces);
 
-    bf16x8 kf[NB][KS];
-    uint64_t ok = 0;  // which of the wavefront's keys exist
-    bool odd_key = false;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      const int j = kw + 32 * i + n;
-      const int64_t off = j < tk.n ? row_offset(g, b, j) : -1;
-      ok |= (__ballot(off >= 0) & 0xffffffffull) << (32 * i);
-      const char* row = g.plane[0] + max(off, (int64_t)0);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const int ch = 16 * s + 8 * gh;
-        u32x4 x;
-        if constexpr (Q4) {
-          const uint32_t codes = *reinterpret_cast<const uint32_t*>(row + h * (D / 2) + ch / 2);
-          const uint8_t byte = (uint8_t)row[g.H * (D / 2) + h * (D / 32) + ch / 32];
-          x = decode8(codes, block_scale(byte));
-        } else {
-          x = *reinterpret_cast<const u32x4*>(row + (h * D + ch) * 2);
-        }
-        if (off < 0) x = u32x4{0, 0, 0, 0};
-        kf[i][s] = as_bf16x8(x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd_key |= word_not_finite(x[e]);
-      }
-    }
-    odd_key = __any(odd_key);  // (0 times one of its channels may be NaN)
-
     // A tile's rows: tokens from c on, heads of the group from g on.
     struct Rows {
       int c, g;
@@ -145,8 +117,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       const int c = token_of(row);
       q_off[i] = (int)((c * a.q.ld_tok + (row - c * per) * a.q.ld_head) * 2) + lane % RC * 16;
     }
-    // A tile's rows pass through registers: LDS that loads fill by themselves would
-    // be read only when they have all arrived, the next tile's among them.
+    // A tile's rows pass through registers (straight to LDS, where rows that are
+    // not there could not be made zeros, they take as long: 1.41 ms for the chunk of
+    // 4096 over 16k slots either way).
     u32x4 raw[NI];
     auto fetch = [&](Rows x) {
       const char* base = a.q.base + (b * a.q.ld_seq + x.c * a.q.ld_tok + (h * a.G + x.g) * a.q.ld_head) * 2;
@@ -190,6 +163,41 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
         s_lim[buf][my_row] = counts ? old + x.c + my_c + 1 : 0;
       }
     };
+
+    // (the first rows are on their way while the keys' places are looked up)
+    Rows now = rows_of(t0);
+    float lse = 0.f;
+    if (t0 < t1) {
+      fetch(now);
+      lse = load_lse(now);
+    }
+    bf16x8 kf[NB][KS];
+    uint64_t ok = 0;  // which of the wavefront's keys exist
+    bool odd_key = false;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const int j = kw + 32 * i + n;
+      const int64_t off = j < tk.n ? row_offset(g, b, j) : -1;
+      ok |= (__ballot(off >= 0) & 0xffffffffull) << (32 * i);
+      const char* row = g.plane[0] + max(off, (int64_t)0);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const int ch = 16 * s + 8 * gh;
+        u32x4 x;
+        if constexpr (Q4) {
+          const uint32_t codes = *reinterpret_cast<const uint32_t*>(row + h * (D / 2) + ch / 2);
+          const uint8_t byte = (uint8_t)row[g.H * (D / 2) + h * (D / 32) + ch / 32];
+          x = decode8(codes, block_scale(byte));
+        } else {
+          x = *reinterpret_cast<const u32x4*>(row + (h * D + ch) * 2);
+        }
+        if (off < 0) x = u32x4{0, 0, 0, 0};
+        kf[i][s] = as_bf16x8(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) odd_key |= word_not_finite(x[e]);
+      }
+    }
+    odd_key = __any(odd_key);  // (0 times one of its channels may be NaN)
 
     float sum[NB][16];
 #pragma unroll
@@ -266,12 +274,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     };
 
     if (t0 < t1) {
-      Rows now = rows_of(t0);
-      fetch(now);
-      put_lse(now, 0, load_lse(now));
+      put_lse(now, 0, lse);
       store(now, 0);
       Rows next = t0 + 1 < t1 ? after(now) : now;
-      float lse = load_lse(next);
+      lse = load_lse(next);
       __syncthreads();
       int buf = 0;
       for (int t = t0; t < t1; ++t) {
