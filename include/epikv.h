@@ -855,7 +855,9 @@ typedef struct epikv_weigh_io {
 } epikv_weigh_io;
 
 /* Device scratch of epikv_attend_weigh with page tables of ld_pt entries
- * (0: none needed, or invalid arguments). */
+ * (0: none needed, or invalid arguments).  With few query rows (chunk times the
+ * query heads of a KV head, 16 at most) it holds their scores: 4 bytes for
+ * every counted query head of a token and every slot that the tables cover. */
 size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads, int64_t ld_pt,
                                           int32_t watch);
 

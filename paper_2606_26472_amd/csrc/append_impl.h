@@ -113,8 +113,8 @@ __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv,
 }
 
 // Bound by HBM (long chunks: 205 MB in 36.6 us, 5.6 TB/s; 182 MB
-// with 4-bit rows 37.7 us) or by the launch and
-// the chain of loads to a row (single tokens: 4.5 us).
+// with 4-bit rows 37.7 us; by positions on three axes 44.3) or by the launch and
+// the chain of loads to a row (single tokens: 4.3 us, on three axes 5.0).
 //
 // Queries: a thread per two vectors of UQ heads (rope_items), in the first
 // nq_blocks workgroups; keys and values: a thread per 8 channels of UKV heads.

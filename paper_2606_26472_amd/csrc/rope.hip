@@ -56,7 +56,8 @@ __global__ __launch_bounds__(256) void k_rope_axes_table(RopeAxesTableArgs a) {
 // 16384 tokens of 32 heads of 128, 44.6 and 45.7 against 43.5 in float32.)
 //
 // Bound by HBM: every byte of x once and of y once, past the caches; 6.1 TB/s
-// there.
+// there.  By positions on three axes the turns come through LDS: 16384 tokens of
+// 32 heads of 128 42.7 us, 6.3 TB/s, as by one; 32 single tokens 3.9 us, 3.3 by one.
 template <bool FP32, bool WAVE, class Args>
 __global__ __launch_bounds__(256) void k_rope(Args a, int per) {
   const Place at = place_of<WAVE>(linear_block(), per, (int64_t)a.B * a.C);

@@ -9,6 +9,14 @@
 // bit): lane (n, g) = (lane % 32, lane / 32) has query row n's scores of keys
 // 8i + 4g + 0..3, so a row's log-sum is one register a lane, and a key's sum stays
 // in one register a lane from the first row to the last.  Only then do lanes meet.
+//
+// Bound by its instructions at the clock that they leave: an exponential, two
+// multiply-adds' worth and their share of the matrix instructions a score.  4096
+// tokens of 32 heads of 128 over 16k slots 542-572 us, 0.84-0.89 PFLOP/s at
+// 2.1-2.2 GHz, matrix cores busy 38 % of the time and vector units 57 %; 8 chunks
+// of 128 over 32k slots in 4 bits 405-430 us, 28 % and 58 %.
+// (A v_mfma alone takes 33 clocks there, with its four multiply-adds and two
+// exponentials 45-49.)
 #include <type_traits>
 
 #include "attend_impl.h"
@@ -18,6 +26,7 @@ namespace {
 
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef uint16_t uint16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
 // Blocks of 32 keys that a wavefront holds (two of 256 channels spill).
@@ -40,16 +49,30 @@ struct WeighPlan {
   float* part;           // [pieces][B][H][ld]
 };
 
-// The sum over the 32 lanes of a half, on each of them (by register moves: as
-// shuffles the 32 sums of a wavefront took 7 us of every workgroup's time).
-__device__ __forceinline__ float half_sum(float v) {
-  const uint32_t w = __float_as_uint(v);
-  const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
-  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  v += dpp_move<0x128>(v);                   // row_ror:8
-  v += dpp_move<0x1B>(dpp_move<0x141>(v));   // row_half_mirror, quad_perm [3,2,1,0]: ^ 4
-  v += dpp_move<0x4E>(v);                    // quad_perm [2,3,0,1]
-  return v + dpp_move<0xB1>(v);              // quad_perm [1,0,3,2]
+// Two values' sums over pairs of lanes that a move exchanges: of the first on
+// the lanes below, of the second on those above (`up`).
+template <int MOVE>
+__device__ __forceinline__ float fold(float a, float b, bool up) {
+  return (up ? b : a) + dpp_move<MOVE>(up ? a : b);
+}
+
+// Sums over the 32 lanes of a half: lane n gets that of value n % K.  Each step
+// halves the lanes of a sum and the values of a lane.
+template <int K>
+__device__ __forceinline__ float half_sums(const float (&v)[K], int n) {
+  float x[16];
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[k]), __float_as_uint(v[k + (K - 16)]), false, false);
+    x[k] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = fold<0x128>(x[k], x[k + 8], n & 8);  // row_ror:8
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] = fold<0x141>(x[k], x[k + 4], n & 4);  // row_half_mirror (lane ^ 7)
+#pragma unroll
+  for (int k = 0; k < 2; ++k) x[k] = fold<0x4E>(x[k], x[k + 2], n & 2);   // quad_perm [2,3,0,1]
+  return fold<0xB1>(x[0], x[1], n & 1);                                   // quad_perm [1,0,3,2]
 }
 
 template <int D, bool Q4>
@@ -173,7 +196,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     }
     bf16x8 kf[NB][KS];
     uint64_t ok = 0;  // which of the wavefront's keys exist
-    bool odd_key = false;
+    uint16x2 top = {0, 0};  // of the magnitudes' bits, or of the blocks' scales
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
       const int j = kw + 32 * i + n;
@@ -188,16 +211,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
           const uint32_t codes = *reinterpret_cast<const uint32_t*>(row + h * (D / 2) + ch / 2);
           const uint8_t byte = (uint8_t)row[g.H * (D / 2) + h * (D / 32) + ch / 32];
           x = decode8(codes, block_scale(byte));
+          top[0] = max(top[0], byte);
         } else {
           x = *reinterpret_cast<const u32x4*>(row + (h * D + ch) * 2);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(uint16x2, x[e] & 0x7fff7fffu));
         }
         if (off < 0) x = u32x4{0, 0, 0, 0};
         kf[i][s] = as_bf16x8(x);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) odd_key |= word_not_finite(x[e]);
       }
     }
-    odd_key = __any(odd_key);  // (0 times one of its channels may be NaN)
+    // 0 times one of its channels may be NaN.  (6 * 2^(252 - 127) is finite still,
+    // and past it blocks may be; a key that is not there may be one, too.)
+    const bool odd_key = __any(max(top[0], top[1]) >= (Q4 ? 253 : 0x7f80));
 
     float sum[NB][16];
 #pragma unroll
@@ -303,19 +329,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
         for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(odd[i][e], held_scale, held_neg));
     }
 
-    // Over the 32 rows' lanes; then key 8(e/4) + 4gh + e%4 of block i is written
-    // by lane e of its half.
+    // Over the 32 rows' lanes: value 16 i + e, of key 8(e/4) + 4gh + e%4 of block
+    // i, to lane n.
+    float all[16 * NB];
+#pragma unroll
+    for (int u = 0; u < 16 * NB; ++u) all[u] = sum[u / 16][u % 16];
+    const float mine = half_sums(all, n);
     float* out = p.part + (((int64_t)piece * g.B + b) * g.H + h) * p.ld + kw;
-#pragma unroll
-    for (int i = 0; i < NB; ++i) {
-      float mine = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float v = half_sum(sum[i][e]);
-        if (n == e) mine = v;
-      }
-      if (n < 16) out[32 * i + 8 * (n / 4) + 4 * gh + n % 4] = mine;
-    }
+    if (n < 16 * NB) out[32 * (n / 16) + 8 * (n % 16 / 4) + 4 * gh + n % 4] = mine;
   }
 }
 

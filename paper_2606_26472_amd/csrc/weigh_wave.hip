@@ -5,6 +5,12 @@
 // together.  One launch then joins the shares and, in workgroups of their own
 // that make the rows' log-sums from the shares' once more, turns the scores to
 // weights and adds them up.
+//
+// The walk is bound by HBM still, its writes at a quarter of the reads' rate: 32
+// sequences of 8k-32k slots (8 KV heads of 128, 4 query heads each) 470 us, 406
+// without the scores (84 MB beside 2.69 GB); in 4 bits 166, 138.  The sums there
+// 20.7 us after the join's 5.7 (4.0 TB/s), one sequence of 4224 slots 7.9 with it
+// (the join alone 5.6): latency.
 #include "attend_wave_impl.h"
 
 namespace epikv {

@@ -458,6 +458,55 @@ def test_other_streams_and_graphs(E, fmt, C):
             assert all(same(a, b) for a, b in zip(fresh, got))
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("C", [1, 5, 48])
+def test_two_calls_at_once(E, fmt, C):
+    """On two streams, a workspace each, over the same pages: what each gives
+    alone."""
+    rng = np.random.default_rng(4)
+    B, Hq, H, d = 2, 8, 2, 128
+    n = [C + 4000, C + 900]
+    c = Cache(E, rng, E.KV_BF16 if fmt == "bf16" else E.KV_MXFP4, B, H, d, 16, max(n))
+    fill(c, rng, n, H, d)
+    need, nd = E.attend_weigh_workspace_bytes(c.cfg, C, Hq, c.ld_pt), ints(n)
+    calls = []
+    for _ in range(2):
+        q = torch.randn(B, C, Hq, d, device=DEV).bfloat16()
+        want = torch.zeros(B, max(n), device=DEV)
+        run(E, c, C, n, q, weights=want)
+        got, ws = torch.zeros_like(want), torch.empty(need, dtype=torch.uint8, device=DEV)
+        io = E.make_attend_io(C, c.pool, 0, c.table, c.ld_pt, nd, q, torch.empty_like(q), workspace=ws, workspace_bytes_=need)
+        calls.append((want, got, io, E.make_weigh_io(got, max(n)), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for _, _, io, wio, s in calls:
+            E.epikv_attend_weigh(c.cfg, io, wio, stream=s)
+    torch.cuda.synchronize()
+    for want, got, *_ in calls:
+        assert same(want, got)
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("C", [1, 48])
+def test_shared_pages(E, fmt, C):
+    """Sequences with the same pages, and one page twice in a table: every slot
+    has its own sum."""
+    rng = np.random.default_rng(14)
+    Hq, H, d, page = 8, 2, 64, 16
+    n = C + 77
+    c = Cache(E, rng, E.KV_BF16 if fmt == "bf16" else E.KV_MXFP4, 2, H, d, page, n)
+    fill(c, rng, [n, n], H, d)
+    q = torch.randn(1, C, Hq, d, device=DEV).bfloat16().expand(2, C, Hq, d)
+    both = c.table[:1].expand(2, -1).contiguous()
+    w = torch.zeros(2, n, device=DEV)
+    run(E, c, C, [n, n], q, table=both, weights=w)
+    assert same(w[0], w[1])
+    twice = both.clone()
+    twice[:, 1] = twice[:, 0]
+    run(E, c, C, [n, n], q, table=twice, weights=w)
+    assert same(w[:, :page], w[:, page:2 * page]) and same(w[0], w[1])
+
+
 def test_wide_tables(E):
     """A page table that covers far more than the sequences hold; what the
     scratch is indexed by passes 32 bits."""
