@@ -14,7 +14,7 @@
 // multiply-adds' worth and their share of the matrix instructions a score.  4096
 // tokens of 32 heads of 128 over 16k slots 542-572 us, 0.84-0.89 PFLOP/s at
 // 2.1-2.2 GHz, matrix cores busy 38 % of the time and vector units 57 %; 8 chunks
-// of 128 over 32k slots in 4 bits 405-430 us, 28 % and 58 %.
+// of 128 over 32k slots in 4 bits 385-400 us, 31 % and 54 %.
 // (A v_mfma alone takes 33 clocks there, with its four multiply-adds and two
 // exponentials 45-49.)
 #include <type_traits>

@@ -9,7 +9,7 @@
 // The walk is bound by HBM still, its writes at a quarter of the reads' rate: 32
 // sequences of 8k-32k slots (8 KV heads of 128, 4 query heads each) 470 us, 406
 // without the scores (84 MB beside 2.69 GB); in 4 bits 166, 138.  The sums there
-// 20.7 us after the join's 5.7 (4.0 TB/s), one sequence of 4224 slots 7.9 with it
+// 17.7 us after the join's 5.9 (4.8 TB/s), one sequence of 4224 slots 8.0 with it
 // (the join alone 5.6): latency.
 #include "attend_wave_impl.h"
 
@@ -68,13 +68,16 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int first = max(0, t.nn - w.watch) * a.G;      // rows of a KV head that count: [first, nn * G)
   const int per_head = t.nn * a.G - first, rows = per_head * g.H;
+  // (rows are divided by 16 at most: one division here, a product each)
+  const uint32_t inverse = 0xffffffffu / (uint32_t)per_head + 1u, inverse_g = 0xffffffffu / (uint32_t)a.G + 1u;
+  auto head_of = [&](int row) { return per_head == 1 ? row : (int)__umulhi((uint32_t)row, inverse); };
   const int2 place = SHARES ? p.shares[b] : make_int2(0, 1);
   const int j = j0 + 4 * lane;
   const bool some = j < t.n;  // (scores are there to the end of a unit)
   const float* kept = p.kept + p.kept_at(b, 0, j / kUnit, a.G, g.H) + j % kUnit;
   const int64_t per_kv_head = p.kept_at(0, 1, 0, a.G, g.H);
   auto lse_at = [&](int h, int r) {
-    const int c = r / a.G, hq = h * a.G + (r - c * a.G);
+    const int c = a.G == 1 ? r : (int)__umulhi((uint32_t)r, inverse_g), hq = h * a.G + (r - c * a.G);
     return a.lse[((int64_t)b * a.heads + hq) * g.C + c] * kLog2e;
   };
   // (a workgroup has a thread for every slot; the old sum is on its way meanwhile)
@@ -91,7 +94,7 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
       while (lanes < 64 && 2 * lanes * min(rows, kWeighRows) <= (int)blockDim.x) lanes *= 2;
       if (at) __syncthreads();
       for (int i = threadIdx.x / lanes; i < n; i += blockDim.x / lanes) {
-        const int h = (at + i) / per_head, r = first + (at + i) - h * per_head;
+        const int h = head_of(at + i), r = first + (at + i) - h * per_head;
         const int part = threadIdx.x & (lanes - 1);
         // (whole: the walk wrote it)
         const float lse = place.y == 1 ? lse_at(h, r) : lse_of_shares(a, p, b, h, r, place, part, lanes);
@@ -104,8 +107,10 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
       float lse[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
-        const int k = min(i + u * waves, n - 1), h = (at + k) / per_head, r = at + k - h * per_head;
-        if (some) x[u] = *reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit);
+        const int k = min(i + u * waves, n - 1), h = head_of(at + k), r = at + k - h * per_head;
+        // (they are not read again; that and the products in the divisions' place: 32
+        // sequences in 4 bits 191.4 -> 190.0 us, in bf16 496 -> 493.5)
+        if (some) x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit));
         lse[u] = SHARES ? lds.lse[k] : lse_at(h, first + r);
       }
 #pragma unroll
