@@ -75,8 +75,15 @@ __device__ __forceinline__ float half_sums(const float (&v)[K], int n) {
   return fold<0xB1>(x[0], x[1], n & 1);                                   // quad_perm [1,0,3,2]
 }
 
+// The same number, what is made of it to be made anew (kept from tile to tile it
+// takes the registers of a third wavefront).
+__device__ __forceinline__ int anew(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 template <int D, bool Q4>
-__global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
   constexpr int NB = key_blocks(D), kKeys = 32 * NB, kSlots = slots_of_group(D);
   constexpr uint64_t kAllKeys = NB == 2 ? ~0ull : 0xffffffffull;
   constexpr int KS = D / 16;            // instructions of a product
@@ -138,48 +145,51 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     for (int i = 0; i < NI; ++i) {
       const int row = wave * (kRows / kWaves) + i * RPI + lane / RC;
       const int c = token_of(row);
-      q_off[i] = (int)((c * a.q.ld_tok + (row - c * per) * a.q.ld_head) * 2) + lane % RC * 16;
+      q_off[i] = (int)((c * a.q.ld_tok + (row - c * per) * a.q.ld_head) * 2) + row_chunk<D>(row, lane % RC) * 16;
     }
-    // A tile's rows pass through registers (straight to LDS, where rows that are
-    // not there could not be made zeros, they take as long: 1.41 ms for the chunk of
-    // 4096 over 16k slots either way).
-    u32x4 raw[NI];
-    auto fetch = [&](Rows x) {
+    // A tile's rows, straight to LDS; the first, which always is there, for one that
+    // is not.
+    auto fetch = [&](Rows x, int buf) {
       const char* base = a.q.base + (b * a.q.ld_seq + x.c * a.q.ld_tok + (h * a.G + x.g) * a.q.ld_head) * 2;
-      const bool plain = p.near && whole(x);
+      char* to = s_q[buf] + wave * (kRows / kWaves) * D * 2;
+      auto load = [&](const char* from, int i) {
+        __builtin_amdgcn_global_load_lds(
+            (const __attribute__((address_space(1))) uint32_t*)(uintptr_t)from,
+            (__attribute__((address_space(3))) uint32_t*)(uint32_t)(uintptr_t)(lds_char*)(to + i * 1024), 16, 0, 0);
+      };
+      if (p.near && whole(x)) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        int64_t off = (uint32_t)q_off[i];
-        if (!plain) {
-          __builtin_amdgcn_sched_barrier(0);
-          const int row = wave * (kRows / kWaves) + i * RPI + lane / RC, c = token_of(row), gr = row - c * per;
-          off = lane % RC * 16;
-          if (has_row(x, c, gr)) off += (c * a.q.ld_tok + gr * a.q.ld_head) * 2;  // (else another is read, and not used)
+        for (int i = 0; i < NI; ++i) load(base + (uint32_t)anew(q_off[i]), i);
+      } else {
+        const int l = anew(lane);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const int row = wave * (kRows / kWaves) + i * RPI + l / RC, c = token_of(row), gr = row - c * per;
+          int64_t off = row_chunk<D>(row, l % RC) * 16;
+          if (has_row(x, c, gr)) off += (c * a.q.ld_tok + gr * a.q.ld_head) * 2;
+          load(base + off, i);
         }
-        raw[i] = *reinterpret_cast<const u32x4*>(base + off);
       }
     };
-    auto store = [&](Rows x, int buf) {
-      const bool all = whole(x);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int row = wave * (kRows / kWaves) + i * RPI + lane / RC;
-        // (a row that is not there: scores of 0, but with an odd key)
-        if (!all && !has_row(x, token_of(row), row - token_of(row) * per)) raw[i] = u32x4{0, 0, 0, 0};
-        *reinterpret_cast<u32x4*>(s_q[buf] + row * D * 2 + row_chunk<D>(row, lane % RC) * 16) = raw[i];
-      }
+    auto tile_sync = [&] {
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
     };
     // The rows' log-sums, some of a tile by every wavefront: loaded two tiles ahead,
     // put to LDS one ahead (and nothing is done with them before, or every tile
     // waits for its load).
     constexpr int RW = kRows / kWaves;
-    const int my_row = wave * RW + (lane & (RW - 1)), my_c = token_of(my_row), my_g = my_row - my_c * per;
     auto load_lse = [&](Rows x) {
+      const int my_row = wave * RW + (anew(lane) & (RW - 1)), my_c = token_of(my_row), my_g = my_row - my_c * per;
       const float* base = a.lse + ((int64_t)b * a.heads + h * a.G + x.g) * g.C + x.c;
       return base[has_row(x, my_c, my_g) ? my_g * g.C + my_c : 0];
     };
     auto put_lse = [&](Rows x, int buf, float lse) {
-      if (lane < RW) {
+      const int l = anew(lane);
+      if (l < RW) {
+        const int my_row = wave * RW + l, my_c = token_of(my_row), my_g = my_row - my_c * per;
         const bool there = has_row(x, my_c, my_g);
         const bool counts = there && row_counts(lse);
         s_neg[buf][my_row] = counts ? -lse * kLog2e : there ? kNotCounted : kNegInf;
@@ -191,7 +201,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     Rows now = rows_of(t0);
     float lse = 0.f;
     if (t0 < t1) {
-      fetch(now);
+      fetch(now, 0);
       lse = load_lse(now);
     }
     bf16x8 kf[NB][KS];
@@ -199,7 +209,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     uint16x2 top = {0, 0};  // of the magnitudes' bits, or of the blocks' scales
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-      const int j = kw + 32 * i + n;
+      const int l = anew(lane), gh = l >> 5, j = kw + 32 * i + (l & 31);
       const int64_t off = j < tk.n ? row_offset(g, b, j) : -1;
       ok |= (__ballot(off >= 0) & 0xffffffffull) << (32 * i);
       const char* row = g.plane[0] + max(off, (int64_t)0);
@@ -232,101 +242,79 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
       for (int e = 0; e < 16; ++e) sum[i][e] = 0.f;
     const uint32_t q_base = (uint32_t)(uintptr_t)(lds_char*)&s_q[0][0] + n * D * 2 + row_chunk<D>(n, gh) * 16;
 
-    // Scores of 32 rows on their way to the sums: the matrix instructions of the
-    // next 32 rows are issued between the exponentials of these.  A score x adds
-    // 2^(x * held_scale + held_neg).
-    f32x16 even[NB], odd[NB];
-    float held_scale = 0.f, held_neg = kNegInf;  // (nothing is held yet)
-#pragma unroll
-    for (int i = 0; i < NB; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) odd[i][e] = 0.f;
-    // Scores of the rows at LDS address `at` and, an instruction's share at a
-    // time, the held ones' weights to the sums.
-    auto products = [&](uint32_t at, f32x16 (&s)[NB], const f32x16 (&held)[NB]) {
-      constexpr int EACH = 16 * NB / KS;  // weights a step
-      constexpr int AHEAD = 2;            // steps that operands are read ahead
+    // The weights of 32 rows to the sums: the scores, and then 2^(scale * x + plus)
+    // of each; the other wavefronts' matrix instructions run beside a wavefront's
+    // exponentials.  (Two wavefronts of a SIMD that each mix theirs, twice the
+    // scores in registers: 1466 us for the chunk of 4096 over 16k slots, attention
+    // and all, 1426 so.)
+    auto rows32 = [&](uint32_t at, int buf, int r, bool all, auto meanwhile) {
+      constexpr int AHEAD = 2;  // steps that operands are read ahead
       auto read = [&](int k) { return as_bf16x8(*(const lds_u32x4*)(uintptr_t)(at ^ (32 * k))); };
       bf16x8 q[KS];
+      f32x16 s[NB];
 #pragma unroll
       for (int k = 0; k < AHEAD; ++k) q[k] = read(k);
-      float x[2][EACH];
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
         if (k + AHEAD < KS) q[k + AHEAD] = read(k + AHEAD);
 #pragma unroll
         for (int i = 0; i < NB; ++i)
           s[i] = mfma32(kf[i][k], q[k], k ? s[i] : f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-        for (int u = 0; u < EACH; ++u) {
-          const int o = k * EACH + u;
-          x[k % 2][u] = exp2_fast(fmaf(held[o / 16][o % 16], held_scale, held_neg));
-        }
-        // (a step later, when they are there)
-        if (k > 0) {
-#pragma unroll
-          for (int u = 0; u < EACH; ++u) sum[((k - 1) * EACH + u) / 16][((k - 1) * EACH + u) % 16] += x[(k - 1) % 2][u];
-        }
-        // (steps stay apart: left to itself the compiler gathers the exponentials
-        // where the sums are next needed)
         __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int u = 0; u < EACH; ++u) sum[((KS - 1) * EACH + u) / 16][((KS - 1) * EACH + u) % 16] += x[(KS - 1) % 2][u];
-#pragma unroll
-      for (int u = 0; u < 16 * NB; ++u) asm volatile("" : "+v"(sum[u / 16][u % 16]));
-    };
-    auto rows32 = [&](uint32_t at, int buf, int r, bool all, f32x16 (&s)[NB], const f32x16 (&held)[NB]) {
-      products(at, s, held);
-      const float neg = s_neg[buf][32 * r + n];
-      held_scale = a.scale2;
-      held_neg = neg;
-      if (all && !__any(fabsf(neg) > kLargeLse && (odd_key || neg != kNegInf))) return;
-      // Hidden keys, rows that do not count, rows whose weights are held to 1: the
-      // exponents here, one by one (all at once they take 60 registers more).
+      const float neg = s_neg[buf][32 * r + n], first_neg = s_neg[buf][0];
       const int lim = s_lim[buf][32 * r + n];
+      __builtin_amdgcn_sched_barrier(0);
+      meanwhile();
+      // Hidden keys, rows that do not count, rows whose weights are held to 1 (and,
+      // with a key or a first row that is not finite, rows that are not there): the
+      // exponents here, one by one.
+      float scale = a.scale2, plus = neg;
+      const bool odd = !all || __any(fabsf(neg) > kLargeLse && (odd_key || neg != kNegInf || fabsf(first_neg) > kLargeLse));
+      if (__builtin_amdgcn_readfirstlane((int)odd)) {  // (one branch for the wavefront)
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const uint32_t mine = ((uint32_t)(ok >> (32 * i)) & below(lim - kw - 32 * i)) >> (4 * gh);
+        for (int i = 0; i < NB; ++i) {
+          const uint32_t mine = ((uint32_t)(ok >> (32 * i)) & below(lim - kw - 32 * i)) >> (4 * (anew(lane) >> 5));
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float y = fmaf(s[i][e], a.scale2, neg);
-          s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? fminf(y, 0.f) : kNegInf;
-          __builtin_amdgcn_sched_barrier(0);
+          for (int e = 0; e < 16; ++e) {
+            const float y = fmaf(s[i][e], a.scale2, neg);
+            s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? fminf(y, 0.f) : kNegInf;
+            __builtin_amdgcn_sched_barrier(0);
+          }
         }
-      }
-      held_scale = 1.f;
-      held_neg = 0.f;
-    };
-
-    if (t0 < t1) {
-      put_lse(now, 0, lse);
-      store(now, 0);
-      Rows next = t0 + 1 < t1 ? after(now) : now;
-      lse = load_lse(next);
-      __syncthreads();
-      int buf = 0;
-      for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) {
-          put_lse(next, buf ^ 1, lse);
-          fetch(next);
-        }
-        const Rows then = t + 2 < t1 ? after(next) : next;
-        lse = load_lse(then);
-        const bool all = ok == kAllKeys && old + now.c + 1 >= kw + kKeys;  // every row sees every key
-        const uint32_t at = q_base + buf * (kRows * D * 2);
-        rows32(at, buf, 0, all, even, odd);
-        rows32(at + 64 * D, buf, 1, all, odd, even);
-        if (t + 1 < t1) store(next, buf ^ 1);
-        buf ^= 1;
-        now = next;
-        next = then;
-        __syncthreads();
+        scale = 1.f;
+        plus = 0.f;
       }
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(odd[i][e], held_scale, held_neg));
+        for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(s[i][e], scale, plus));
+#pragma unroll
+      for (int u = 0; u < 16 * NB; ++u) asm volatile("" : "+v"(sum[u / 16][u % 16]));
+    };
+
+    if (t0 < t1) {
+      put_lse(now, 0, lse);
+      Rows next = t0 + 1 < t1 ? after(now) : now;
+      lse = load_lse(next);
+      tile_sync();
+      int buf = 0;
+      for (int t = t0; t < t1; ++t) {
+        if (t + 1 < t1) put_lse(next, buf ^ 1, lse);
+        const Rows then = t + 2 < t1 ? after(next) : next;
+        const bool all = ok == kAllKeys && old + now.c + 1 >= kw + kKeys;  // every row sees every key
+        const uint32_t at = q_base + buf * (kRows * D * 2);
+        rows32(at, buf, 0, all, [] {});
+        rows32(at + 64 * D, buf, 1, all, [&] {
+          // (when this tile's rows have been read: a read waits for whatever is on its way to LDS)
+          if (t + 1 < t1) fetch(next, buf ^ 1);
+          lse = load_lse(then);
+        });
+        buf ^= 1;
+        now = next;
+        next = then;
+        tile_sync();
+      }
     }
 
     // Over the 32 rows' lanes: value 16 i + e, of key 8(e/4) + 4gh + e%4 of block
@@ -334,6 +322,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void k_weigh_tile(AttendArgs a, Wei
     float all[16 * NB];
 #pragma unroll
     for (int u = 0; u < 16 * NB; ++u) all[u] = sum[u / 16][u % 16];
+    const int l = anew(lane), n = l & 31, gh = l >> 5;
     const float mine = half_sums(all, n);
     float* out = p.part + (((int64_t)piece * g.B + b) * g.H + h) * p.ld + kw;
     if (n < 16 * NB) out[32 * (n / 16) + 8 * (n % 16 / 4) + 4 * gh + n % 4] = mine;
