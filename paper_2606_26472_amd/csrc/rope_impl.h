@@ -65,7 +65,7 @@ struct TableRow {
 // Positions on several axes: every pair is in the row of its axis' position.
 // WAVE: the wavefront has one token; its pairs come into LDS, one a lane, and
 // from there to the lanes as from a row of the table.  (Pair by pair from the
-// table, eight loads a lane, 16384 tokens of 32 heads of 128 took 66 us.)
+// table, eight loads a lane, 16384 tokens of 32 heads of 128 take 57 us, so 42.6.)
 template <bool WAVE>
 struct TableRows {
   static constexpr bool STAGED = WAVE;
@@ -95,7 +95,9 @@ struct TableRows {
     return word;
   }
   __device__ __forceinline__ float2 entry(const RopeAxesArg& r, uint32_t axis, int i) const {
-    const uint32_t lo = axis & 1u ? p[1] : p[0], hi = axis & 1u ? p[3] : p[2];
+    // (all four read first: as a choice of what to read the compiler puts them in LDS)
+    const uint32_t p0 = p[0], p1 = p[1], p2 = p[2], p3 = p[3];
+    const uint32_t lo = axis & 1u ? p1 : p0, hi = axis & 1u ? p3 : p2;
     return r.table[(uint64_t)(axis & 2u ? hi : lo) * ((uint32_t)r.r / 2) + (uint32_t)i];
   }
   // All lanes of the wavefront that have an item (its first ones), before load.
@@ -261,11 +263,12 @@ __device__ __forceinline__ Place place_of(int64_t block, int per, int64_t tokens
 
 // Whether a token's items go to wavefronts of their own: where they fill them,
 // and with positions on several axes (whose turns come through LDS then) where
-// more than half of the lanes have one.  Tokens of 24 heads of 64, 96 items: 37 us
-// so, 60 without; of 9, 36 items: 23, 38; of 5, 20 items: 37, 35; appended with 32
-// items of queries and 32 of keys and values: 71, 62.
+// more than two thirds of the lanes have one.  16384 tokens of 24 heads of 64, 96
+// items: 22 us so, 28 without; of 14, 56 items: 13.7, 16.5; of 9 of 128, 72 items:
+// 30.5, 19.3; of 9 of 64, 36 items: 11.7, 12.7; of 9 of 128 in float32, 144 items:
+// 32.1, 29.7.
 inline bool by_wave(const RopeArg&, int per) { return per % 64 == 0; }
-inline bool by_wave(const RopeAxesArg&, int per) { return 2 * per > (per + 63) / 64 * 64; }
+inline bool by_wave(const RopeAxesArg&, int per) { return 3 * per > 2 * ((per + 63) / 64 * 64); }
 inline int64_t threads_of(int64_t tokens, int per, bool wave) { return tokens * (wave ? (per + 63) / 64 * 64 : per); }
 
 // Threads beyond 2^32 do not fit place_of's numbers.

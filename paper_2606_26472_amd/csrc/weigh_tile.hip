@@ -10,13 +10,12 @@
 // 8i + 4g + 0..3, so a row's log-sum is one register a lane, and a key's sum stays
 // in one register a lane from the first row to the last.  Only then do lanes meet.
 //
-// Bound by its instructions at the clock that they leave: an exponential, two
-// multiply-adds' worth and their share of the matrix instructions a score.  4096
-// tokens of 32 heads of 128 over 16k slots 542-572 us, 0.84-0.89 PFLOP/s at
-// 2.1-2.2 GHz, matrix cores busy 38 % of the time and vector units 57 %; 8 chunks
-// of 128 over 32k slots in 4 bits 385-400 us, 31 % and 54 %.
-// (A v_mfma alone takes 33 clocks there, with its four multiply-adds and two
-// exponentials 45-49.)
+// Bound by its instructions at the clock that they leave: an exponential, a
+// multiply-add, an addition and their share of the matrix instructions a score.
+// 4096 tokens of 32 heads of 128 over 16k slots 482-505 us, 0.95-1.0 PFLOP/s at
+// 2.0 GHz, matrix cores busy 46 % of the time and vector units 68 %; 8 chunks of
+// 128 over 32k slots in 4 bits 326-358 us, 35 % and 64 %.  (15 % fewer clocks, with
+// a third wavefront to a SIMD, were 8 % of the time: the clock fell by 7 %.)
 #include <type_traits>
 
 #include "attend_impl.h"
