@@ -9,7 +9,7 @@
 // The walk is bound by HBM still, its writes at a quarter of the reads' rate: 32
 // sequences of 8k-32k slots (8 KV heads of 128, 4 query heads each) 470 us, 406
 // without the scores (84 MB beside 2.69 GB); in 4 bits 166, 138.  The sums there
-// 17.7 us after the join's 5.9 (4.8 TB/s), one sequence of 4224 slots 8.0 with it
+// 17.7 us after the join's 5.9 (4.8 TB/s), one sequence of 4224 slots 7.0 with it
 // (the join alone 5.6): latency.
 #include "attend_wave_impl.h"
 
@@ -26,10 +26,13 @@ struct WeighScratch {
   __attribute__((aligned(16))) float sums[8][kWeighSlots];
 };
 
-// The log-sum of one row from its shares, by `lanes` lanes that each take some.
+// The log-sum of one row from its shares, by `lanes` lanes that each take some, two
+// at a time.  (A launch fetches its instructions anew, and more of them cost more
+// than loads that wait for each other: one sequence of 4224 slots 14.4 us so, 14.9
+// with four at a time, 15.5 with eight; so it is with the rows below.)
 __device__ __forceinline__ float lse_of_shares(const AttendArgs& a, const WavePlan& p, int b, int h, int r,
                                                int2 place, int part, int lanes) {
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 2;
   const int64_t from = ((int64_t)(place.x + b) * a.pg.H + h) * a.R + r, step = (int64_t)a.pg.H * a.R;
   float top = kNegInf, s = 0.f;
   for (int k = part; k < place.y; k += AHEAD * lanes) {
@@ -61,7 +64,7 @@ __device__ __forceinline__ float lse_of_shares(const AttendArgs& a, const WavePl
 template <bool SHARES>
 __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, int b,
                                             int tile, const SeqTokens& t, WeighScratch& lds) {
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = SHARES ? 4 : 8;  // rows of a wavefront on their way
   const PagedArgs& g = a.pg;
   const int j0 = tile * kWeighSlots;
   const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
@@ -177,8 +180,8 @@ int units_in(int slots) { return (slots + kUnit - 1) / kUnit; }
 
 // Tiles of all sequences up to which their log-sums are made beside the join, in
 // every tile's workgroup anew; more wait for it.  A launch less against that work:
-// one sequence of 32k slots 32.2 us beside, 35.3 after; of 64k 61.4, 61.3; of 128k
-// 111.0, 105.8.
+// one sequence of 32k slots 31.6 us beside, 35.1 after; of 64k 60.9, 61.0; of 128k
+// 108.7, 105.7.
 constexpr int kMergeTiles = 256;
 
 template <int D>
