@@ -64,12 +64,12 @@ __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv,
       raise_flag(g.status, b);  // (no place for its id: a step would move one that was never set)
   }
   f32x4 cs[4];
-  if (a.rope.table && __any(rot)) turns.stage(a.rope);
+  if constexpr (decltype(turns)::STAGED)
+    if (a.rope.table && __any(rot)) turns.stage(a.rope);
   if (rot) {
-    if (half)
-      turns.template load<8>(a.rope, first * 8, cs);
-    else
-      turns.template load<4>(a.rope, vec * 4, cs);
+    const int pair = half ? first * 8 : vec * 4;
+    turns.template load<4>(a.rope, pair, cs);
+    if (half) turns.template load<4>(a.rope, pair + 4, cs + 2);
   }
   char* row = g.plane[kv] + off;
 #pragma unroll

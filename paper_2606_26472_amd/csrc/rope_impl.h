@@ -207,12 +207,8 @@ __device__ __forceinline__ void rope_items(const RowsArg& x, const RowsArg& y, c
   f32x4 cs[N / 2];
   if (rot) {
     // (N pairs together, or half of them for each vector)
-    if (r.interleaved) {
-      turns.template load<N / 2>(r, lo / 2, cs);
-      turns.template load<N / 2>(r, hi / 2, cs + N / 4);
-    } else {
-      turns.template load<N>(r, lo, cs);
-    }
+    turns.template load<N / 2>(r, r.interleaved ? lo / 2 : lo, cs);
+    turns.template load<N / 2>(r, r.interleaved ? hi / 2 : lo + N / 2, cs + N / 4);
   }
 #pragma unroll
   for (int k = 0; k < U; ++k) {
