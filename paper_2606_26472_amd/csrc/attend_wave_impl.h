@@ -593,16 +593,23 @@ constexpr int64_t kCacheBytes = 128 << 20;
 // much, their counts say.
 template <int D, bool Q4, bool LARGE, bool KEEP>
 __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs a, WavePlan p) {
-  // (as many as the workgroup has wavefronts: Scratch, then with KEEP the scores)
-  extern __shared__ __align__(16) char s_dynamic[];
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const PagedArgs& g = a.pg;
   const int h = blockIdx.y * p.hw + wave;
   const int64_t team = linear_block();
   if (h >= g.H || team >= p.n_teams) return;
-  Scratch<D, Q4>& lds = reinterpret_cast<Scratch<D, Q4>*>(s_dynamic)[wave];
-  float* keep = reinterpret_cast<float*>(s_dynamic + p.hw * sizeof(Scratch<D, Q4>)) + (KEEP ? wave * kKeepFloats<D, Q4> : 0);
+  Scratch<D, Q4>* scratch;
+  float* keep = nullptr;
+  if constexpr (KEEP) {  // (as many as the workgroup has wavefronts: Scratch, then the scores)
+    extern __shared__ __align__(16) char s_dynamic[];
+    scratch = reinterpret_cast<Scratch<D, Q4>*>(s_dynamic);
+    keep = reinterpret_cast<float*>(s_dynamic + p.hw * sizeof(Scratch<D, Q4>)) + wave * kKeepFloats<D, Q4>;
+  } else {
+    __shared__ Scratch<D, Q4> s_scratch[D == 256 ? 4 : 8];
+    scratch = s_scratch;
+  }
+  Scratch<D, Q4>& lds = scratch[wave];
   Share x;
   if (!p.split) {  // a sequence to a team
     x.b = (int)team;
@@ -773,7 +780,7 @@ template <int D, bool KEEP>
 hipError_t launch_shares(const AttendArgs& a, const WavePlan& p, bool q4, hipStream_t s) {
   const dim3 grid = linear_grid(p.n_teams, p.hw * 64, (a.pg.H + p.hw - 1) / p.hw);
   const dim3 block(p.hw * 64);
-  const auto lds = [&](size_t scratch, int floats) { return (unsigned)(p.hw * (scratch + (KEEP ? floats * 4 : 0))); };
+  const auto lds = [&](size_t scratch, int floats) { return KEEP ? (unsigned)(p.hw * (scratch + floats * 4)) : 0u; };
   if (q4)
     hipLaunchKernelGGL((k_attend_wave<D, true, false, KEEP>), grid, block,
                        lds(sizeof(Scratch<D, true>), kKeepFloats<D, true>), s, a, p);
