@@ -323,6 +323,31 @@ def test_nan_and_infinity_that_are_seen(E, C, n):
     check(E, "bf16", 4, C, 4, 2, 128, 16, [n] * 4, edit=edit)
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("heads", [(3, 1, 64), (10, 2, 128), (7, 1, 256), (65, 1, 64), (8, 2, 128)])
+@pytest.mark.parametrize("C,every", [(1, 1), (3, 2), (80, 9), (80, 21), (80, 79)])
+def test_bad_queries_beside_good_ones(E, fmt, heads, C, every):
+    """Groups that do not fill a tile's rows, and tokens whose first head holds a
+    NaN or an infinity, a tile's first row among them: the others' weights are
+    whole."""
+    Hq, H, d = heads
+    fm = E.KV_BF16 if fmt == "bf16" else E.KV_MXFP4
+    rng = np.random.default_rng(C + every)
+    n = [C + 700, C]
+    c = Cache(E, rng, fm, 2, H, d, 16, max(n))
+    held = fill(c, rng, n, H, d)
+    q, q64 = bf16(rng.standard_normal((2, C, Hq, d)))
+    for t in (q, q64):
+        t[:, ::every, 0, 1] = float("nan")
+        t[1, ::every, 0, 2:] = float("inf")
+    w = torch.zeros(2, max(n), device=DEV)
+    run(E, c, C, n, q, weights=w)
+    for b in range(2):
+        with np.errstate(invalid="ignore"):
+            want, tol = expected(q64[b], *held[b], C, d ** -0.5, None, 1.0, 0.0, 1.0, 0)
+        assert np.isfinite(want).all() and np.all(np.abs(f64(w)[b, :n[b]] - want) <= tol), b
+
+
 @pytest.mark.parametrize("C", [1, 3, 40])
 def test_rows_that_see_only_minus_infinity(E, C):
     """Every score -infinity: nothing is added, and no NaN."""
