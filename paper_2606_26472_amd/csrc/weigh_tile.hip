@@ -16,8 +16,6 @@
 // 2.0 GHz, matrix cores busy 46 % of the time and vector units 68 %; 8 chunks of
 // 128 over 32k slots in 4 bits 326-358 us, 35 % and 64 %.  (15 % fewer clocks, with
 // a third wavefront to a SIMD, were 8 % of the time: the clock fell by 7 %.)
-#include <type_traits>
-
 #include "attend_impl.h"
 
 namespace epikv {
@@ -390,8 +388,9 @@ WeighPlan weigh_plan(int B, int H, int G, int d, int slots, int watch) {
   const int64_t blocks = (int64_t)B * H * p.slot_tiles;
   // Pieces: of two tiles at least while they give every compute unit its two
   // workgroups, of eight where there are more (what a workgroup takes to begin and
-  // to end is worth about two).  512 tokens alone 65 us in pieces of eight, 53 of
-  // two; 4 chunks of 100 over 4096 slots 101 us in pieces of two, 90 in one.
+  // to end is worth about two).  512 tokens alone 51.5 us
+  // so, 59.9 without pieces of two; 2048 alone 105 so, 118 with pieces of two
+  // throughout.
   const auto pieces = [&](int64_t least, int64_t most) { return std::min(row_tiles / least, most / blocks); };
   p.pieces = (int)std::max<int64_t>(
       1, std::min<int64_t>(kMaxPieces, std::max(pieces(2, 2 * cus), pieces(8, 8 * cus))));
