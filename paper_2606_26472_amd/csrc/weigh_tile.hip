@@ -388,9 +388,8 @@ WeighPlan weigh_plan(int B, int H, int G, int d, int slots, int watch) {
   const int64_t blocks = (int64_t)B * H * p.slot_tiles;
   // Pieces: of two tiles at least while they give every compute unit its two
   // workgroups, of eight where there are more (what a workgroup takes to begin and
-  // to end is worth about two).  512 tokens alone 51.5 us
-  // so, 59.9 without pieces of two; 2048 alone 105 so, 118 with pieces of two
-  // throughout.
+  // to end is worth about two).  512 tokens alone 51.5 us so, 59.9 without pieces
+  // of two; 2048 alone 105 so, 118 with pieces of two throughout.
   const auto pieces = [&](int64_t least, int64_t most) { return std::min(row_tiles / least, most / blocks); };
   p.pieces = (int)std::max<int64_t>(
       1, std::min<int64_t>(kMaxPieces, std::max(pieces(2, 2 * cus), pieces(8, 8 * cus))));
