@@ -99,10 +99,31 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // NaN in sums that go on for good.
 __device__ __forceinline__ bool row_counts(float lse) { return fabsf(lse) < -kNegInf; }
 
-// A row's weight of a slot from its score and its log-sum to the base 2.  One
-// at most: what both were rounded to may leave more where they are large.
-__device__ __forceinline__ float weight_of(float score, float scale2, float lse2) {
-  return exp2_fast(fminf(fmaf(score, scale2, -lse2), 0.f));
+// What makes weights of a row's scores: the maximum (base 2) that its sum was taken
+// from, and 1 / sum; {0, 0} for a row that does not count.  Not the log-sum, whose
+// own rounding, 2^-24 of it, would be an error of every weight: 1 % where scores are
+// 1e5, factors where they are 1e7.
+__device__ __forceinline__ float2 norm_of(float top, float sum, float lse) {
+  return row_counts(lse) ? make_float2(top, 1.f / sum) : make_float2(0.f, 0.f);
+}
+
+// A row's weight of a slot.  (The product with the scale is not rounded before the
+// maximum is off.)
+__device__ __forceinline__ float weight_of(float score, float scale2, float2 norm) {
+  const float w = exp2_fast(fmaf(score, scale2, -norm.x)) * norm.y;
+  return norm.y != 0.f ? w : 0.f;  // (the score may be NaN)
+}
+
+// A row's log-sum, and its norm, where they are asked for.  some: the sum is not 0.
+// NORMS: the kernel is asked for norms at all.
+template <bool NORMS>
+__device__ __forceinline__ void write_log_sum(const AttendArgs& a, int b, int hq, int c, float top, float sum,
+                                              bool some) {
+  if (!a.lse && !(NORMS && a.norms)) return;
+  const int64_t at = ((int64_t)b * a.heads + hq) * a.pg.C + c;
+  const float lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+  if (a.lse) a.lse[at] = lse;
+  if (NORMS && a.norms) a.norms[at] = norm_of(top, sum, lse);
 }
 
 // A slot's sum: what is kept of the old one and this call's.  j < ld_s.
@@ -125,7 +146,7 @@ size_t weigh_wave_workspace(int B, int H, int R, int d, int G, int slots, int wa
 hipError_t launch_weigh_wave(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 size_t attend_tile_workspace(int B, int H, int R, int d);
 size_t weigh_tile_workspace(int B, int H, int G, int d, int slots, int watch);
-// After the attention, whose log-sums are in a.lse.
+// After the attention, which left a.norms.
 hipError_t launch_weigh_tile(const AttendArgs& a, const WeighArgs& w, bool q4, void* ws, hipStream_t s);
 hipError_t launch_attend_tile(const AttendArgs& a, bool q4, void* ws, hipStream_t s);
 

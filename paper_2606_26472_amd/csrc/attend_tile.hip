@@ -395,9 +395,7 @@ __global__ __launch_bounds__(64 * W, D == 256 ? 1 : 2) void k_attend_tile(Attend
         }
         *reinterpret_cast<u32x2*>(op + (32 * j + 8 * i) * 2) = w;
       }
-    if (a.lse && gh == 0)
-      a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
-          some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+    if (gh == 0) write_log_sum<true>(a, b, hq, c, top, sum, some);
   } else if (real) {
     const int64_t at = (((int64_t)piece * g.B + b) * g.H + h) * a.R + r;
     if (gh == 0) p.part_ml[at] = make_float2(top, sum);
@@ -466,9 +464,7 @@ __global__ __launch_bounds__(256) void k_attend_tile_join(AttendArgs a, TilePlan
   u32x2 w = {0u, 0u};
   if (some) w = u32x2{pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
   *reinterpret_cast<u32x2*>(a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head) * 2 + 8 * x) = w;
-  if (a.lse && x == 0)
-    a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
-        some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+  if (x == 0) write_log_sum<true>(a, b, hq, c, top, sum, some);
 }
 
 // Pieces of a row tile at most.  How long the sequences are only the device

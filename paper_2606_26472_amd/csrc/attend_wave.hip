@@ -8,7 +8,7 @@ namespace {
 template <int D>
 __global__ __launch_bounds__(512) void k_attend_join(AttendArgs a, WavePlan p) {
   __shared__ JoinScratch<D> lds;
-  join_row<D>(a, p, linear_block(), lds);
+  join_row<D, false>(a, p, linear_block(), lds);
 }
 
 template <int D>

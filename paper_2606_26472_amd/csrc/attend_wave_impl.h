@@ -496,9 +496,7 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan
         }
         *reinterpret_cast<u32x2*>(op + (VC * i + j) * 2) = w;
       }
-    if (a.lse && q4 == 0)
-      a.lse[((int64_t)b * a.heads + hq) * g.C + c] =
-          some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+    if (q4 == 0) write_log_sum<KEEP>(a, b, hq, c, top, sum, some);
   } else if (real) {
     const int64_t at = ((int64_t)slot * g.H + h) * a.R + r;
     float* po = p.part_o + at * D + (D / 4) * q4;
@@ -513,14 +511,14 @@ __device__ __forceinline__ void attend_share(const AttendArgs& a, const WavePlan
 }
 
 // The outputs of a sequence with nothing to see.
-template <int D>
+template <int D, bool KEEP>
 __device__ void attend_nothing(const AttendArgs& a, int b, int h, int lane) {
   for (int i = lane; i < a.R * (D / 8); i += 64) {
     const int r = i / (D / 8), x = i - r * (D / 8);
     const int c = r / a.G, hq = h * a.G + (r - c * a.G);
     *reinterpret_cast<u32x4*>(a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head + x * 8) * 2) =
         u32x4{0, 0, 0, 0};
-    if (a.lse && x == 0) a.lse[((int64_t)b * a.heads + hq) * a.pg.C + c] = kNegInf;
+    if (x == 0) write_log_sum<KEEP>(a, b, hq, c, kNegInf, 0.f, false);
   }
 }
 
@@ -618,7 +616,7 @@ __global__ __launch_bounds__(D == 256 ? 256 : 512) void k_attend_wave(AttendArgs
     x.before = x.lo = 0;
     x.hi = units_of(x.t);
     if (x.hi == 0) {
-      attend_nothing<D>(a, x.b, h, lane);
+      attend_nothing<D, KEEP>(a, x.b, h, lane);
       return;
     }
   } else if (g.B <= 64) {
@@ -662,7 +660,7 @@ struct JoinScratch {
 // trips (a pass for the maximum and one for the sums took a third).  5.4 us
 // for 132 shares of 32 rows and for 32 sequences of 8 shares each, 1.5 of them
 // the launch.
-template <int D>
+template <int D, bool KEEP>
 __device__ __forceinline__ void join_row(const AttendArgs& a, const WavePlan& p, int64_t row, JoinScratch<D>& lds) {
   constexpr int E = D / 64, AHEAD = 16;
   float (&s_o)[8][D] = lds.o;
@@ -681,12 +679,11 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const WavePlan& p,
   if (t.bad && threadIdx.x == 0 && hr == 0) raise_flag(g.status, b);
   const int c = r / a.G, hq = h * a.G + (r - c * a.G);
   char* op = a.out.base + (b * a.out.ld_seq + c * a.out.ld_tok + hq * a.out.ld_head) * 2;
-  float* lse = a.lse ? a.lse + ((int64_t)b * a.heads + hq) * g.C + c : nullptr;
   const bool any = units_of(t) > 0;
   if (any && place.y == 1) return;  // written whole
   if (!any || r >= t.nn * a.G) {
     if (threadIdx.x < D / 8) reinterpret_cast<u32x4*>(op)[threadIdx.x] = u32x4{0, 0, 0, 0};
-    if (lse && threadIdx.x == 0) *lse = kNegInf;
+    if (threadIdx.x == 0) write_log_sum<KEEP>(a, b, hq, c, kNegInf, 0.f, false);
     return;
   }
   const int n = place.y;
@@ -750,7 +747,7 @@ __device__ __forceinline__ void join_row(const AttendArgs& a, const WavePlan& p,
   const bool some = sum != 0.f;
   const float inv = 1.f / sum;
   reinterpret_cast<uint32_t*>(op)[threadIdx.x] = some ? pack_bf16(x * inv, y * inv) : 0u;
-  if (lse && threadIdx.x == 0) *lse = some ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : kNegInf;
+  if (threadIdx.x == 0) write_log_sum<KEEP>(a, b, hq, c, top, sum, some);
 }
 
 // Wavefronts resident per SIMD that the shares are counted for.

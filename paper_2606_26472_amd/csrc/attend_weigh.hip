@@ -3,7 +3,7 @@
 //   weights[b][j] = keep * old[b][j] + gain * sum exp(scale * (q . k_j) - lse)
 //
 // over the counted rows (tokens times query heads) that see slot j.  The sums
-// need every row's final log-sum, so they are taken after the attention: from
+// need every row's final maximum and sum, so they are taken after the attention: from
 // scores that it kept where rows are few (weigh_wave.hip), from scores made
 // again where they are many (weigh_tile.hip).
 #include "attend_impl.h"
@@ -18,16 +18,16 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t attend_weigh_workspace(int B, int C, int H, int heads, int d, int slots, int watch) {
   const int G = heads / H, R = C * G;
   if (R <= kWaveRows) return weigh_wave_workspace(B, H, R, d, G, slots, watch);
-  return round256((size_t)B * C * heads * sizeof(float)) +
+  return round256((size_t)B * C * heads * sizeof(float2)) +
          std::max(attend_tile_workspace(B, H, R, d), weigh_tile_workspace(B, H, G, d, slots, watch));
 }
 
 hipError_t launch_attend_weigh(const AttendArgs& args, const WeighArgs& w, bool q4, void* ws, hipStream_t s) {
   if (args.R <= kWaveRows) return launch_weigh_wave(args, w, q4, ws, s);
   AttendArgs a = args;
-  if (!a.lse) a.lse = (float*)ws;
+  a.norms = (float2*)ws;
   // (the attention is done with its workspace when the sums begin)
-  void* rest = (char*)ws + round256((size_t)a.pg.B * a.pg.C * a.heads * sizeof(float));
+  void* rest = (char*)ws + round256((size_t)a.pg.B * a.pg.C * a.heads * sizeof(float2));
   const hipError_t e = launch_attend_tile(a, q4, rest, s);
   return e != hipSuccess ? e : launch_weigh_tile(a, w, q4, rest, s);
 }

@@ -566,6 +566,7 @@ struct AttendArgs {
   PagedArgs pg;
   RowsArg q, out;
   float* lse;
+  float2* norms;                           // [B][heads][C] (or nullptr): attend_impl.h, norm_of
   int32_t heads, G, R;                     // query heads; per KV head; rows C * G
   float scale2;                            // scale * log2(e)
 };

@@ -1,17 +1,17 @@
 // The sums of many query rows' weights per slot (prefill, long chunks), after
 // the attention itself.
 //
-// A row's weights need its log-sum, which is known when the attention ends, so
+// A row's weights need its maximum and sum, known when the attention ends, so
 // the scores are made a second time: a wavefront keeps 64 keys (32 of 256
 // channels) of a KV head in registers, as the first operand of v_mfma 32x32x16,
 // and the query rows stream past through LDS, 64 at a time and two tiles deep.
 // S^T = K Q^T, in the attention's order of channels (the same scores, bit for
 // bit): lane (n, g) = (lane % 32, lane / 32) has query row n's scores of keys
-// 8i + 4g + 0..3, so a row's log-sum is one register a lane, and a key's sum stays
+// 8i + 4g + 0..3, so a row's norm is two registers a lane, and a key's sum stays
 // in one register a lane from the first row to the last.  Only then do lanes meet.
 //
-// Bound by its instructions at the clock that they leave: an exponential, a
-// multiply-add, an addition and their share of the matrix instructions a score.
+// Bound by its instructions at the clock that they leave: an exponential, two
+// multiply-adds and their share of the matrix instructions a score.
 // 4096 tokens of 32 heads of 128 over 16k slots 482-505 us, 0.95-1.0 PFLOP/s at
 // 2.0 GHz, matrix cores busy 46 % of the time and vector units 68 %; 8 chunks of
 // 128 over 32k slots in 4 bits 326-358 us, 35 % and 64 %.  (15 % fewer clocks, with
@@ -31,8 +31,6 @@ constexpr int key_blocks(int d) { return d == 256 ? 1 : 2; }
 constexpr int slots_of_group(int d) { return kWaves * 32 * key_blocks(d); }
 constexpr int kRows = 64;                  // query rows of a tile, at most
 constexpr int kMaxPieces = 64;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLargeLse = 65536.f;       // from 2^16 on weights are held to 1 one by one
 
 // How the work is dealt out: the slots of every (sequence, KV head) in tiles,
 // each tile's rows in `pieces`.
@@ -80,7 +78,7 @@ __device__ __forceinline__ int anew(int x) {
 }
 
 template <int D, bool Q4>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : D == 64 ? 4 : 3) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
   constexpr int NB = key_blocks(D), kKeys = 32 * NB, kSlots = slots_of_group(D);
   constexpr uint64_t kAllKeys = NB == 2 ? ~0ull : 0xffffffffull;
   constexpr int KS = D / 16;            // instructions of a product
@@ -88,7 +86,8 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
   constexpr int RPI = 1024 / (D * 2);   // rows a load of a wavefront
   constexpr int NI = kRows / kWaves / RPI;
   __shared__ __align__(1024) char s_q[2][kRows * D * 2];
-  __shared__ float s_neg[2][kRows];  // minus a row's log-sum (minus infinity: no such row)
+  __shared__ float s_neg[2][kRows];  // minus a row's maximum (minus infinity: no such row)
+  __shared__ float s_inv[2][kRows];  // 1 / its sum
   constexpr float kNotCounted = -kNegInf;
   __shared__ int s_lim[2][kRows];    // the slots that it sees
   const PagedArgs& g = a.pg;
@@ -174,32 +173,33 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
     };
-    // The rows' log-sums, some of a tile by every wavefront: loaded two tiles ahead,
+    // The rows' norms, some of a tile by every wavefront: loaded two tiles ahead,
     // put to LDS one ahead (and nothing is done with them before, or every tile
     // waits for its load).
     constexpr int RW = kRows / kWaves;
-    auto load_lse = [&](Rows x) {
+    auto load_norm = [&](Rows x) {
       const int my_row = wave * RW + (anew(lane) & (RW - 1)), my_c = token_of(my_row), my_g = my_row - my_c * per;
-      const float* base = a.lse + ((int64_t)b * a.heads + h * a.G + x.g) * g.C + x.c;
+      const float2* base = a.norms + ((int64_t)b * a.heads + h * a.G + x.g) * g.C + x.c;
       return base[has_row(x, my_c, my_g) ? my_g * g.C + my_c : 0];
     };
-    auto put_lse = [&](Rows x, int buf, float lse) {
+    auto put_norm = [&](Rows x, int buf, float2 norm) {
       const int l = anew(lane);
       if (l < RW) {
         const int my_row = wave * RW + l, my_c = token_of(my_row), my_g = my_row - my_c * per;
         const bool there = has_row(x, my_c, my_g);
-        const bool counts = there && row_counts(lse);
-        s_neg[buf][my_row] = counts ? -lse * kLog2e : there ? kNotCounted : kNegInf;
+        const bool counts = there && norm.y != 0.f;
+        s_neg[buf][my_row] = counts ? -norm.x : there ? kNotCounted : kNegInf;
+        s_inv[buf][my_row] = counts ? norm.y : 0.f;
         s_lim[buf][my_row] = counts ? old + x.c + my_c + 1 : 0;
       }
     };
 
     // (the first rows are on their way while the keys' places are looked up)
     Rows now = rows_of(t0);
-    float lse = 0.f;
+    float2 norm = {0.f, 0.f};
     if (t0 < t1) {
       fetch(now, 0);
-      lse = load_lse(now);
+      norm = load_norm(now);
     }
     bf16x8 kf[NB][KS];
     uint64_t ok = 0;  // which of the wavefront's keys exist
@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
       for (int e = 0; e < 16; ++e) sum[i][e] = 0.f;
     const uint32_t q_base = (uint32_t)(uintptr_t)(lds_char*)&s_q[0][0] + n * D * 2 + row_chunk<D>(n, gh) * 16;
 
-    // The weights of 32 rows to the sums: the scores, and then 2^(scale * x + plus)
+    // The weights of 32 rows to the sums: the scores, and then 2^(scale * x + plus) / sum
     // of each; the other wavefronts' matrix instructions run beside a wavefront's
     // exponentials.  (Two wavefronts of a SIMD that each mix theirs, twice the
     // scores in registers: 1466 us for the chunk of 4096 over 16k slots, attention
@@ -259,15 +259,14 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
           s[i] = mfma32(kf[i][k], q[k], k ? s[i] : f32x16{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f});
         __builtin_amdgcn_sched_barrier(0);
       }
-      const float neg = s_neg[buf][32 * r + n], first_neg = s_neg[buf][0];
+      const float neg = s_neg[buf][32 * r + n], first_neg = s_neg[buf][0], inv = s_inv[buf][32 * r + n];
       const int lim = s_lim[buf][32 * r + n];
       __builtin_amdgcn_sched_barrier(0);
       meanwhile();
-      // Hidden keys, rows that do not count, rows whose weights are held to 1 (and,
-      // with a key or a first row that is not finite, rows that are not there): the
-      // exponents here, one by one.
+      // Hidden keys, rows that do not count (and, with a key or a first row that is
+      // not finite, rows that are not there): the exponents here, one by one.
       float scale = a.scale2, plus = neg;
-      const bool odd = !all || __any(fabsf(neg) > kLargeLse && (odd_key || neg != kNegInf || fabsf(first_neg) > kLargeLse));
+      const bool odd = !all || __any(neg == kNotCounted || (neg == kNegInf && (odd_key || first_neg == kNotCounted)));
       if (__builtin_amdgcn_readfirstlane((int)odd)) {  // (one branch for the wavefront)
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -275,7 +274,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             const float y = fmaf(s[i][e], a.scale2, neg);
-            s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? fminf(y, 0.f) : kNegInf;
+            s[i][e] = mine >> (8 * (e / 4) + e % 4) & 1u ? y : kNegInf;
             __builtin_amdgcn_sched_barrier(0);
           }
         }
@@ -285,19 +284,19 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
 #pragma unroll
       for (int i = 0; i < NB; ++i)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) sum[i][e] += exp2_fast(fmaf(s[i][e], scale, plus));
+        for (int e = 0; e < 16; ++e) sum[i][e] = fmaf(exp2_fast(fmaf(s[i][e], scale, plus)), inv, sum[i][e]);
 #pragma unroll
       for (int u = 0; u < 16 * NB; ++u) asm volatile("" : "+v"(sum[u / 16][u % 16]));
     };
 
     if (t0 < t1) {
-      put_lse(now, 0, lse);
+      put_norm(now, 0, norm);
       Rows next = t0 + 1 < t1 ? after(now) : now;
-      lse = load_lse(next);
+      norm = load_norm(next);
       tile_sync();
       int buf = 0;
       for (int t = t0; t < t1; ++t) {
-        if (t + 1 < t1) put_lse(next, buf ^ 1, lse);
+        if (t + 1 < t1) put_norm(next, buf ^ 1, norm);
         const Rows then = t + 2 < t1 ? after(next) : next;
         const bool all = ok == kAllKeys && old + now.c + 1 >= kw + kKeys;  // every row sees every key
         const uint32_t at = q_base + buf * (kRows * D * 2);
@@ -305,7 +304,7 @@ __global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : 3) void k_weigh_tile(At
         rows32(at + 64 * D, buf, 1, all, [&] {
           // (when this tile's rows have been read: a read waits for whatever is on its way to LDS)
           if (t + 1 < t1) fetch(next, buf ^ 1);
-          lse = load_lse(then);
+          norm = load_norm(then);
         });
         buf ^= 1;
         now = next;

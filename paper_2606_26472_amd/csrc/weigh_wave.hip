@@ -3,8 +3,8 @@
 // The walk keeps its scores (attend_wave_impl.h): 4 bytes a row and slot, where
 // the keys they come from have 256 (128 channels in bf16) for a KV head's rows
 // together.  One launch then joins the shares and, in workgroups of their own
-// that make the rows' log-sums from the shares' once more, turns the scores to
-// weights and adds them up.
+// that make the rows' maxima and sums from the shares' once more, turns the scores
+// to weights and adds them up.
 //
 // The walk is bound by HBM still, its writes at a quarter of the reads' rate: 32
 // sequences of 8k-32k slots (8 KV heads of 128, 4 query heads each) 470 us, 406
@@ -16,22 +16,21 @@
 namespace epikv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kWeighSlots = 256;   // of a workgroup, four to a lane
-constexpr int kWeighRows = 512;    // rows whose log-sums a workgroup holds at a time
+constexpr int kWeighRows = 512;    // rows whose norms a workgroup holds at a time
 constexpr int kMaxTiles = 16384;   // workgroups, about; each goes on to further slots
 
 struct WeighScratch {
-  float lse[kWeighRows];                       // base 2
+  float2 norm[kWeighRows];
   __attribute__((aligned(16))) float sums[8][kWeighSlots];
 };
 
-// The log-sum of one row from its shares, by `lanes` lanes that each take some, two
+// What makes weights of one row's scores (norm_of), from its shares, by `lanes` lanes that each take some, two
 // at a time.  (A launch fetches its instructions anew, and more of them cost more
 // than loads that wait for each other: one sequence of 4224 slots 14.4 us so, 14.9
 // with four at a time, 15.5 with eight; so it is with the rows below.)
-__device__ __forceinline__ float lse_of_shares(const AttendArgs& a, const WavePlan& p, int b, int h, int r,
-                                               int2 place, int part, int lanes) {
+__device__ __forceinline__ float2 norm_of_shares(const AttendArgs& a, const WavePlan& p, int b, int h, int r,
+                                                 int2 place, int part, int lanes) {
   constexpr int AHEAD = 2;
   const int64_t from = ((int64_t)(place.x + b) * a.pg.H + h) * a.R + r, step = (int64_t)a.pg.H * a.R;
   float top = kNegInf, s = 0.f;
@@ -55,12 +54,12 @@ __device__ __forceinline__ float lse_of_shares(const AttendArgs& a, const WavePl
     s = s * exp2_fast(top - base2) + s2 * exp2_fast(top2 - base2);
     top = grown;
   }
-  return top + __builtin_amdgcn_logf(s);
+  return norm_of(top, s, (top + __builtin_amdgcn_logf(s)) * kLn2);
 }
 
 // The sums of 256 slots, four to a lane, a workgroup's wavefronts taking turns
-// over the counted rows.  SHARES: the rows' log-sums are made from their shares
-// here; else they are in a.lse.
+// over the counted rows.  SHARES: the rows' norms are made from their shares here;
+// else (and where a row has one share, the whole) they are in a.norms.
 template <bool SHARES>
 __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan& p, const WeighArgs& w, int b,
                                             int tile, const SeqTokens& t, WeighScratch& lds) {
@@ -79,9 +78,9 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
   const bool some = j < t.n;  // (scores are there to the end of a unit)
   const float* kept = p.kept + p.kept_at(b, 0, j / kUnit, a.G, g.H) + j % kUnit;
   const int64_t per_kv_head = p.kept_at(0, 1, 0, a.G, g.H);
-  auto lse_at = [&](int h, int r) {
+  auto norm_at = [&](int h, int r) {
     const int c = a.G == 1 ? r : (int)__umulhi((uint32_t)r, inverse_g), hq = h * a.G + (r - c * a.G);
-    return a.lse[((int64_t)b * a.heads + hq) * g.C + c] * kLog2e;
+    return a.norms[((int64_t)b * a.heads + hq) * g.C + c];
   };
   // (a workgroup has a thread for every slot; the old sum is on its way meanwhile)
   const bool live = threadIdx.x < kWeighSlots && j0 + (int)threadIdx.x < t.n;
@@ -100,33 +99,29 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
         const int h = head_of(at + i), r = first + (at + i) - h * per_head;
         const int part = threadIdx.x & (lanes - 1);
         // (whole: the walk wrote it)
-        const float lse = place.y == 1 ? lse_at(h, r) : lse_of_shares(a, p, b, h, r, place, part, lanes);
-        if (part == 0) lds.lse[i] = lse;
+        const float2 norm = place.y == 1 ? norm_at(h, r) : norm_of_shares(a, p, b, h, r, place, part, lanes);
+        if (part == 0) lds.norm[i] = norm;
       }
       __syncthreads();
     }
     for (int i = wave; i < n; i += AHEAD * waves) {
       f32x4 x[AHEAD];
-      float lse[AHEAD];
+      float2 norm[AHEAD];
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         const int k = min(i + u * waves, n - 1), h = head_of(at + k), r = at + k - h * per_head;
         // (they are not read again; that and the products in the divisions' place: 32
         // sequences in 4 bits 191.4 -> 190.0 us, in bf16 496 -> 493.5)
         if (some) x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit));
-        lse[u] = SHARES ? lds.lse[k] : lse_at(h, first + r);
+        norm[u] = SHARES ? lds.norm[k] : norm_at(h, first + r);
       }
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         if (i + u * waves >= n) continue;
         // (a slot that the row does not see has -infinity.  No branch over rows that
         // do not count: one sequence of 4224 slots 16.1 us so, 17.4 with it)
-        const bool counts = row_counts(lse[u]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = weight_of(x[u][e], a.scale2, lse[u]);
-          sum[e] += counts ? y : 0.f;
-        }
+        for (int e = 0; e < 4; ++e) sum[e] += weight_of(x[u][e], a.scale2, norm[u]);
       }
     }
   }
@@ -163,12 +158,12 @@ __global__ __launch_bounds__(512) void k_join_weigh(AttendArgs a, WavePlan p, We
   } lds;
   const int64_t block = linear_block();
   if (block < n_join)
-    join_row<D>(a, p, block, lds.join);
+    join_row<D, true>(a, p, block, lds.join);
   else
     weigh_tiles<true>(a, p, w, block - n_join, tiles, lds.weigh);
 }
 
-// The sums alone, after a join that leaves every row's log-sum in a.lse.
+// The sums alone, after a join that leaves every row's norm.
 __global__ __launch_bounds__(256) void k_weigh(AttendArgs a, WavePlan p, WeighArgs w, int tiles) {
   __shared__ WeighScratch lds;
   weigh_tiles<false>(a, p, w, linear_block(), tiles, lds);
@@ -178,7 +173,7 @@ size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 int units_in(int slots) { return (slots + kUnit - 1) / kUnit; }
 
-// Tiles of all sequences up to which their log-sums are made beside the join, in
+// Tiles of all sequences up to which their rows' norms are made beside the join, in
 // every tile's workgroup anew; more wait for it.  A launch less against that work:
 // one sequence of 32k slots 31.6 us beside, 35.1 after; of 64k 60.9, 61.0; of 128k
 // 108.7, 105.7.
@@ -207,7 +202,7 @@ hipError_t launch_weigh(const AttendArgs& a, const WavePlan& p, const WeighArgs&
 }  // namespace
 
 size_t weigh_wave_workspace(int B, int H, int R, int d, int G, int slots, int watch) {
-  return round256(attend_wave_workspace(B, H, R, d)) + round256((size_t)B * H * R * sizeof(float)) +
+  return round256(attend_wave_workspace(B, H, R, d)) + round256((size_t)B * H * R * sizeof(float2)) +
          (size_t)B * units_in(slots) * (H * watch * G) * kUnit * sizeof(float);
 }
 
@@ -216,8 +211,8 @@ hipError_t launch_weigh_wave(const AttendArgs& args, const WeighArgs& w, bool q4
   const PagedArgs& g = a.pg;
   WavePlan p = placed_plan(a, ws);
   char* at = (char*)ws + round256(attend_wave_workspace(g.B, g.H, a.R, g.d));
-  if (!a.lse) a.lse = (float*)at;
-  p.kept = (float*)(at + round256((size_t)g.B * g.H * a.R * sizeof(float)));
+  a.norms = (float2*)at;
+  p.kept = (float*)(at + round256((size_t)g.B * g.H * a.R * sizeof(float2)));
   p.units = units_in(g.max_tokens);
   p.watch = w.watch;
   if (g.d == 64) return launch_weigh<64>(a, p, w, q4, s);
