@@ -869,10 +869,10 @@ size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, i
  *                   all query heads h of exp(scale*(q . k_j) - lse[b][h][c])
  * with keep = keep_old, or keep_new for the new tokens' slots; a sum kept by 0
  * is not read, whatever it holds.  A token adds nothing to slots it does not
- * see, and a query head of it nothing at all where its log-sum is not finite
- * (it sees nothing; a NaN or an infinity is among its scores; they pass 2^30,
- * where float32 no longer tells them apart): one bad token does not spoil sums
- * that go on.  Slots in pages out of range get nothing added.  Entries from
+ * see or gives a score of -infinity, and a query head of it nothing at all where
+ * its log-sum is not finite (it sees nothing but such slots; a NaN or +infinity
+ * is among its scores) or is 2^30 or more in magnitude (float32 no longer tells
+ * such scores apart): one bad token does not spoil sums that go on.  Slots in pages out of range get nothing added.  Entries from
  * n_cached[b] on are left as they are, and so is a sequence without new tokens
  * or with counts out of range; a slot >= ld_s has no place (not written; flags
  * the sequence).  Weights and sums are float32, added in a fixed order.

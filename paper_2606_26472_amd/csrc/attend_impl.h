@@ -93,11 +93,11 @@ __device__ __forceinline__ int row_chunk(int row, int c) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Whether a row counts: one that sees nothing, or has a NaN or an infinity among
-// its scores (or scores past 2^30, less exact than their exponentials can bear),
-// has no finite log-sum and adds nothing to any slot, or one token would leave
-// NaN in sums that go on for good.
-__device__ __forceinline__ bool row_counts(float lse) { return fabsf(lse) < -kNegInf; }
+// Whether a row counts.  One that sees nothing, or has a NaN or an infinite score,
+// has no finite log-sum; from 2^30 on a maximum's rounding, 2^-24 of it, is 64 and
+// more, and its exponential passes float32 soon after.  Such a row adds nothing to
+// any slot, or one token would leave NaN in sums that go on for good.
+__device__ __forceinline__ bool row_counts(float lse) { return fabsf(lse) < 0x1p30f; }
 
 // What makes weights of a row's scores: the maximum (base 2) that its sum was taken
 // from, and 1 / sum; {0, 0} for a row that does not count.  Not the log-sum, whose

@@ -99,3 +99,37 @@ def test_weights_of_a_row_add_up_to_one(E, fmt, form, scale):
     rows = C * heads[0]
     off = np.abs(f64(w).sum(1) / rows - 1.0)
     assert off.max() <= 2.0 ** -15 + (max(n) + rows) * 2.0 ** -24, off.max()
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("form", FORMS, ids=lambda f: "x".join(str(x) for x in (f[0],) + f[1] + (max(f[2]), len(f[2]))))
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_rows_past_two_to_the_thirtieth_do_not_count(E, fmt, form, sign):
+    """Every slot's score the same: a row's weights are one over what it sees.
+    Every other query head's log-sum is 0.98 times 2^30 and the rest's 1.96
+    times, then 0.51 and 1.02; the former count, the latter do not.  (No score
+    is rounded; a sum by 2^-24 of itself for each term, and its inverse.)"""
+    C, heads, n = form
+    Hq, H, d = heads
+    rng = np.random.default_rng(5)
+    c = cache_of(E, fmt, rng, C, heads, n)
+
+    def edit(b, k, v):
+        k[:] = 0.0
+        k[:, :, 40] = sign * 2.0 ** 15
+        v[:] = 1.0
+    fill(c, rng, n, H, d, edit)
+    x = np.zeros((len(n), C, Hq, d))
+    x[:, :, 0::2, 40] = 2.0 ** 15
+    x[:, :, 1::2, 40] = 2.0 ** 16
+    q, _ = bf16(x)
+    for scale in (0.98, 0.51):
+        w = no_weights(n)
+        _, lse, _ = run(E, c, C, n, q, weights=w, scale=scale)
+        assert torch.all(lse[:, 0::2].abs() < 2.0 ** 30) and torch.all(lse[:, 1::2].abs() > 2.0 ** 30)
+        assert torch.isfinite(lse).all()
+        w = f64(w)
+        for b in sorted({0, len(n) // 2, len(n) - 1}):
+            seen = n[b] - C + 1 + np.arange(C)
+            want = (Hq // 2) * ((np.arange(n[b])[None] < seen[:, None]) / seen[:, None]).sum(0)
+            assert np.all(np.abs(w[b, :n[b]] - want) <= (2.0 ** -20 + (n[b] + C * Hq) * 2.0 ** -24) * want), (scale, b)
