@@ -150,7 +150,7 @@ int check_cfg(const epikv_cfg* c) {
   if (c->n_kv_heads < 1) return EPIKV_EINVAL_SHAPE;
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return EPIKV_EINVAL_SHAPE;
   const int hd = c->n_kv_heads * c->head_dim;
-  if (hd > 2048) return EPIKV_EINVAL_SHAPE;
+  if (hd > kMaxRowChannels) return EPIKV_EINVAL_SHAPE;
   const int row_vec = hd / 8;
   // One row of one plane is streamed by one wavefront (at most 4 16-byte
   // columns per lane): H*d <= 2048 guarantees it.

@@ -408,6 +408,7 @@ hipError_t launch_compact_inplace(const InplaceArgs& a, hipStream_t s);
 hipError_t launch_fill(const FillArgs& a, hipStream_t s);
 
 // Tunables the host layer validates against.
+constexpr int kMaxRowChannels = 2048;    // KV heads times head_dim, at most
 constexpr int kScoreThreads = 256;
 constexpr int kScoreSeg = 32;            // tokens per score_hs workgroup (wide rows)
 constexpr int kScoreSegMin = 4;          // shortened down to so many tokens

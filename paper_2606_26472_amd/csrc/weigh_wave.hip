@@ -17,7 +17,7 @@ namespace epikv {
 namespace {
 
 constexpr int kWeighSlots = 256;   // of a workgroup, four to a lane
-constexpr int kWeighRows = 512;    // rows whose norms a workgroup holds at a time
+constexpr int kWeighRows = kWaveRows * (kMaxRowChannels / 64);  // that count, of all KV heads, at most
 constexpr int kMaxTiles = 16384;   // workgroups, about; each goes on to further slots
 
 struct WeighScratch {
@@ -88,41 +88,37 @@ __device__ __forceinline__ void weigh_slots(const AttendArgs& a, const WavePlan&
   if (live && !mine) raise_flag(g.status, b);
   const float kept_old = mine ? kept_sum(w, b, j0 + (int)threadIdx.x, t) : 0.f;
   f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int at = 0; at < rows; at += SHARES ? kWeighRows : rows) {
-    const int n = SHARES ? min(kWeighRows, rows - at) : rows;
-    if constexpr (SHARES) {
-      // (as many lanes to a row as the rows leave each, a power of two)
-      int lanes = 1;
-      while (lanes < 64 && 2 * lanes * min(rows, kWeighRows) <= (int)blockDim.x) lanes *= 2;
-      if (at) __syncthreads();
-      for (int i = threadIdx.x / lanes; i < n; i += blockDim.x / lanes) {
-        const int h = head_of(at + i), r = first + (at + i) - h * per_head;
-        const int part = threadIdx.x & (lanes - 1);
-        // (whole: the walk wrote it)
-        const float2 norm = place.y == 1 ? norm_at(h, r) : norm_of_shares(a, p, b, h, r, place, part, lanes);
-        if (part == 0) lds.norm[i] = norm;
-      }
-      __syncthreads();
+  if constexpr (SHARES) {
+    // (as many lanes to a row as the rows leave each, a power of two)
+    int lanes = 1;
+    while (lanes < 64 && 2 * lanes * rows <= (int)blockDim.x) lanes *= 2;
+    for (int i = threadIdx.x / lanes; i < rows; i += blockDim.x / lanes) {
+      const int h = head_of(i), r = first + i - h * per_head;
+      const int part = threadIdx.x & (lanes - 1);
+      // (whole: the walk wrote it)
+      const float2 norm = place.y == 1 ? norm_at(h, r) : norm_of_shares(a, p, b, h, r, place, part, lanes);
+      if (part == 0) lds.norm[i] = norm;
     }
-    for (int i = wave; i < n; i += AHEAD * waves) {
-      f32x4 x[AHEAD];
-      float2 norm[AHEAD];
+    __syncthreads();
+  }
+  for (int i = wave; i < rows; i += AHEAD * waves) {
+    f32x4 x[AHEAD];
+    float2 norm[AHEAD];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int k = min(i + u * waves, n - 1), h = head_of(at + k), r = at + k - h * per_head;
-        // (they are not read again; that and the products in the divisions' place: 32
-        // sequences in 4 bits 191.4 -> 190.0 us, in bf16 496 -> 493.5)
-        if (some) x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit));
-        norm[u] = SHARES ? lds.norm[k] : norm_at(h, first + r);
-      }
+    for (int u = 0; u < AHEAD; ++u) {
+      const int k = min(i + u * waves, rows - 1), h = head_of(k), r = k - h * per_head;
+      // (they are not read again; that and the products in the divisions' place: 32
+      // sequences in 4 bits 191.4 -> 190.0 us, in bf16 496 -> 493.5)
+      if (some) x[u] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(kept + h * per_kv_head + r * kUnit));
+      norm[u] = SHARES ? lds.norm[k] : norm_at(h, first + r);
+    }
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        if (i + u * waves >= n) continue;
-        // (a slot that the row does not see has -infinity.  No branch over rows that
-        // do not count: one sequence of 4224 slots 16.1 us so, 17.4 with it)
+    for (int u = 0; u < AHEAD; ++u) {
+      if (i + u * waves >= rows) continue;
+      // (a slot that the row does not see has -infinity.  No branch over rows that
+      // do not count: one sequence of 4224 slots 16.1 us so, 17.4 with it)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += weight_of(x[u][e], a.scale2, norm[u]);
-      }
+      for (int e = 0; e < 4; ++e) sum[e] += weight_of(x[u][e], a.scale2, norm[u]);
     }
   }
   *reinterpret_cast<f32x4*>(&lds.sums[wave][4 * lane]) = sum;

@@ -27,7 +27,9 @@ def E():
 # of rows, in pieces and not, of every number of channels.
 FORMS = [(1, (8, 2, 64), [40]), (1, (8, 2, 128), [900]), (3, (4, 2, 128), [700, 33]), (1, (4, 1, 256), [5000]),
          (2, (8, 2, 64), [40000, 30000]), (1, (4, 2, 64), [30] * 1100), (40, (8, 2, 64), [40]),
-         (60, (8, 2, 128), [1000, 60]), (30, (4, 1, 256), [600]), (700, (8, 2, 64), [700])]
+         (60, (8, 2, 128), [1000, 60]), (30, (4, 1, 256), [600]), (700, (8, 2, 64), [700]),
+         # (as many rows as a walk can have, 16 of 32 KV heads)
+         (1, (512, 32, 64), [900]), (4, (128, 32, 64), [33, 400])]
 
 
 def cache_of(E, fmt, rng, C, heads, n):
