@@ -857,7 +857,11 @@ typedef struct epikv_weigh_io {
 /* Device scratch of epikv_attend_weigh with page tables of ld_pt entries
  * (0: none needed, or invalid arguments).  With few query rows (chunk times the
  * query heads of a KV head, 16 at most) it holds their scores: 4 bytes for
- * every counted query head of a token and every slot that the tables cover. */
+ * every counted query head of a token and every slot that the tables cover.
+ * With more it holds partial sums, 4 bytes for every KV head of a sequence and
+ * every slot that the tables cover (several of each in small calls), beside
+ * what the attention needs.  Either grows with the tables, whatever the
+ * sequences hold. */
 size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, int32_t n_heads, int64_t ld_pt,
                                           int32_t watch);
 

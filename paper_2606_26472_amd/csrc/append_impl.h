@@ -112,9 +112,12 @@ __device__ __forceinline__ void append_vecs(const Args& a, int b, int c, int kv,
   }
 }
 
-// Bound by HBM (long chunks: 205 MB in 36.6 us, 5.6 TB/s; 182 MB
-// with 4-bit rows 37.7 us; by positions on three axes 44.3) or by the launch and
-// the chain of loads to a row (single tokens: 4.3 us, on three axes 5.0).
+// Bound by HBM where rows are bf16 (long chunks: 205 MB in 36.6 us, 5.6 TB/s).  With
+// 4-bit rows the same chunk's 182 MB take 37.7 us, and by positions on three axes
+// either format 42 to 43.7 (4.9 and 4.2 TB/s): not for their bytes, but for the chain
+// of loads to a row and its turns, for which wavefronts wait 57 to 60 % of their time
+// (vector units are busy 43 to 47 %).  Single tokens: the launch and that chain, 4.3
+// us, on three axes 5.0.
 //
 // Queries: a thread per two vectors of UQ heads (rope_items), in the first
 // nq_blocks workgroups; keys and values: a thread per 8 channels of UKV heads.

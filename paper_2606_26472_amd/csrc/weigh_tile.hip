@@ -12,9 +12,9 @@
 //
 // Bound by its instructions at the clock that they leave: an exponential, two
 // multiply-adds and their share of the matrix instructions a score.
-// 4096 tokens of 32 heads of 128 over 16k slots 482-505 us, 0.95-1.0 PFLOP/s at
-// 2.0 GHz, matrix cores busy 46 % of the time and vector units 68 %; 8 chunks of
-// 128 over 32k slots in 4 bits 326-358 us, 35 % and 64 %.  (15 % fewer clocks, with
+// 4096 tokens of 32 heads of 128 over 16k slots 493-510 us, 0.94-0.97 PFLOP/s at
+// 2.0 GHz, matrix cores busy 45 % of the time and vector units 67 %; 8 chunks of
+// 128 over 32k slots in 4 bits 345-363 us, 34 % and 62 %.  (15 % fewer clocks, with
 // a third wavefront to a SIMD, were 8 % of the time: the clock fell by 7 %.)
 #include "attend_impl.h"
 

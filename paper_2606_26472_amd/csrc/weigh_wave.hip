@@ -9,7 +9,7 @@
 // The walk is bound by HBM still, its writes at a quarter of the reads' rate: 32
 // sequences of 8k-32k slots (8 KV heads of 128, 4 query heads each) 470 us, 406
 // without the scores (84 MB beside 2.69 GB); in 4 bits 166, 138.  The sums there
-// 17.7 us after the join's 5.9 (4.8 TB/s), one sequence of 4224 slots 7.0 with it
+// 17.5 us after the join's 5.7 (4.8 TB/s), one sequence of 4224 slots 7.1 with it
 // (the join alone 5.6): latency.
 #include "attend_wave_impl.h"
 
