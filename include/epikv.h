@@ -876,10 +876,11 @@ size_t epikv_attend_weigh_workspace_bytes(const epikv_cfg* cfg, int32_t chunk, i
  * see or gives a score of -infinity, and a query head of it nothing at all where
  * its log-sum is not finite (it sees nothing but such slots; a NaN or +infinity
  * is among its scores) or is 2^30 or more in magnitude (float32 no longer tells
- * such scores apart): one bad token does not spoil sums that go on.  Slots in pages out of range get nothing added.  Entries from
- * n_cached[b] on are left as they are, and so is a sequence without new tokens
- * or with counts out of range; a slot >= ld_s has no place (not written; flags
- * the sequence).  Weights and sums are float32, added in a fixed order.
+ * such scores apart): one bad token does not spoil sums that go on.  Slots in
+ * pages out of range get nothing added.  Entries from n_cached[b] on are left
+ * as they are, and so is a sequence without new tokens or with counts out of
+ * range; a slot >= ld_s has no place (not written; flags the sequence).
+ * Weights and sums are float32, added in a fixed order.
  * The sums are scores of the slots as epikv_select takes them: added up over
  * the layers, they go to epikv_evict_step (chunk = 0, `scores`), which moves
  * them with the rows.

@@ -93,8 +93,8 @@ __device__ __forceinline__ int row_chunk(int row, int c) {
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Whether a row counts.  One that sees nothing, or has a NaN or an infinite score,
-// has no finite log-sum; from 2^30 on a maximum's rounding, 2^-24 of it, is 64 and
+// Whether a row counts.  One that sees nothing, or has a NaN or +infinity among its
+// scores, has no finite log-sum; from 2^30 on a maximum's rounding, 2^-24 of it, is 64 and
 // more, and its exponential passes float32 soon after.  Such a row adds nothing to
 // any slot, or one token would leave NaN in sums that go on for good.
 __device__ __forceinline__ bool row_counts(float lse) { return fabsf(lse) < 0x1p30f; }

@@ -78,7 +78,8 @@ __device__ __forceinline__ int anew(int x) {
 }
 
 template <int D, bool Q4>
-__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : D == 64 ? 4 : 3) void k_weigh_tile(AttendArgs a, WeighArgs w, WeighPlan p) {
+__global__ __launch_bounds__(64 * kWaves, D == 256 ? 2 : D == 64 ? 4 : 3) void k_weigh_tile(AttendArgs a, WeighArgs w,
+                                                                                            WeighPlan p) {
   constexpr int NB = key_blocks(D), kKeys = 32 * NB, kSlots = slots_of_group(D);
   constexpr uint64_t kAllKeys = NB == 2 ? ~0ull : 0xffffffffull;
   constexpr int KS = D / 16;            // instructions of a product

@@ -25,10 +25,11 @@ struct WeighScratch {
   __attribute__((aligned(16))) float sums[8][kWeighSlots];
 };
 
-// What makes weights of one row's scores (norm_of), from its shares, by `lanes` lanes that each take some, two
-// at a time.  (A launch fetches its instructions anew, and more of them cost more
-// than loads that wait for each other: one sequence of 4224 slots 14.4 us so, 14.9
-// with four at a time, 15.5 with eight; so it is with the rows below.)
+// What makes weights of one row's scores (norm_of), from its shares, by `lanes`
+// lanes that each take some, two at a time.  (A launch fetches its instructions
+// anew, and more of them cost more than loads that wait for each other: one sequence
+// of 4224 slots 14.4 us so, 14.9 with four at a time, 15.5 with eight; so it is with
+// the rows below.)
 __device__ __forceinline__ float2 norm_of_shares(const AttendArgs& a, const WavePlan& p, int b, int h, int r,
                                                  int2 place, int part, int lanes) {
   constexpr int AHEAD = 2;
